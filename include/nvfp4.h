@@ -335,6 +335,109 @@ NVFP4_API int nvfp4_linear_bwd_bf16(const void* dY, const void* W, const void* X
                           void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
+ * FP8 (the 8-bit format that the paper compares FP4 training with), one scale for each block of 128: codes are E4M3 bytes, a
+ * scale is E8M0 (2^(code - 127)), the smallest power of two with 448 * scale >= amax of its block (code 0 for a block of zeros).
+ * Values are multiplied by the reciprocal, which is exact, and rounded to nearest, ties to even.  A block that holds a NaN or an
+ * infinity has scale code 255 (NaN) and NaN codes, and every element of a product computed with it is NaN.
+ *
+ * A quantized row of Kq codes takes Kq rounded up to 16 bytes (the padding is never read), so that Rq and Kq may be any size:
+ * nvfp4_codes_bytes_fp8(Rq, Kq) bytes.  Scales: one byte per row and block of 128, linear [Rq, ceil(Kq/128)] or in the tiles of 128
+ * rows x 4 blocks of nvfp4_quantize (padding zero); nvfp4_sf_bytes_fp8 gives the size of one matrix's.
+ *
+ * nvfp4_quantize_fp8: x holds `batch` matrices of [rows, cols], leading dimension ld, one behind the other (rows * ld elements).
+ *   block_rows 1: blocks of 1 x 128 along the contraction axis of each output;  128: blocks of 128 x 128, for weights: codes_t is
+ *   then the transpose of codes_row.  codes_row / scales_row: Q(x), blocks along cols, [batch, rows, cols]; codes_t / scales_t:
+ *   Q(x^T), blocks along rows, [batch, cols, rows].  Either pair may be NULL; both come from one read.
+ *   Alignment: x and all outputs 16-byte aligned, ld a multiple of 8 elements.
+ * nvfp4_gemm_fp8: D[M,N] = A[M,K] . B[N,K]^T on such codes with swizzled scales, fp32 accumulation, D fp32 or bf16.  Any M, N and K;
+ *   pointers 16-byte aligned, ldd*sizeof(D) a multiple of 16.
+ */
+NVFP4_API size_t nvfp4_codes_bytes_fp8(int64_t Rq, int64_t Kq);
+NVFP4_API size_t nvfp4_sf_bytes_fp8(int64_t Rq, int64_t Kq, int sf_layout);
+NVFP4_API int nvfp4_quantize_fp8(const void* x, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int block_rows,
+                       uint8_t* codes_row, uint8_t* scales_row, uint8_t* codes_t, uint8_t* scales_t, int sf_layout,
+                       void* cuda_stream);
+NVFP4_API int nvfp4_gemm_fp8(const uint8_t* a_codes, const uint8_t* a_sf, const uint8_t* b_codes, const uint8_t* b_sf,
+                   int64_t M, int64_t N, int64_t K, void* d, int d_dtype, int64_t ldd, void* cuda_stream);
+
+/*
+ * The linear layer in FP8 (Eq. 1-3): Y = Q(X) . Q128(W)^T, dX = Q(dY) . Q128(W), dW = Q(dY^T) . Q(X^T)^T, where Q has blocks of 1 x 128
+ * along the contraction axis and Q128 blocks of 128 x 128.  X[M,K], W[N,K], dY[M,N] of `dtype`, all tensors dense and 16-byte aligned;
+ * N and K multiples of 8, M (the tokens) any.  workspace: nvfp4_linear_fp8_workspace_bytes(M, N, K, which) bytes, 256-byte aligned,
+ * contents undefined afterwards; the size query returns 0 for a layer that the calls reject.
+ */
+typedef enum { NVFP4_FP8_FWD = 0, NVFP4_FP8_BWD = 1 } nvfp4_fp8_kind;
+NVFP4_API size_t nvfp4_linear_fp8_workspace_bytes(int64_t M, int64_t N, int64_t K, int which);
+NVFP4_API int nvfp4_linear_fp8_fwd(const void* X, const void* W, int dtype, int64_t M, int64_t N, int64_t K, void* Y, int y_dtype,
+                         void* workspace, size_t workspace_bytes, void* cuda_stream);
+NVFP4_API int nvfp4_linear_fp8_bwd(const void* dY, const void* W, const void* X, int dtype, int64_t M, int64_t N, int64_t K,
+                         void* dX, int dx_dtype, void* dW, int dw_dtype, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Layers whose weights are split among experts: tokens sorted by expert, and back.
+ *
+ * A token has `topk` slots; slot s = token * topk + j names the expert of the token's j-th choice in expert_of (int32, or int64 where
+ * wide == 1; an index outside [0, experts) drops the slot).  The rows of an expert are a segment of R = nvfp4_expert_rows(tokens, topk,
+ * experts) rows (0: refused, also for more than 1024 experts): segment e is [offsets[e], offsets[e + 1]), begins at a multiple of
+ * 128, and holds the expert's slots in ascending order, then padding up to the next multiple of 128.  offsets[experts] rows are
+ * used; the rows behind them are neither read nor written by any call.
+ *
+ * nvfp4_expert_sort: counts [experts] (slots of each expert, without padding), offsets [experts + 1], row_of [tokens * topk] (the
+ *   slot's row, -1: dropped), slot_of [R] (the row's slot, -1: padding and unused rows); all int32.
+ * nvfp4_expert_gather: rows[r] = w * x[token of r's slot], zero in padding; x [tokens, cols] with leading dimension ld, rows [R, cols].
+ *   weights [tokens, topk] of weights_dtype, or NULL for 1.  Its gradient by x is nvfp4_expert_combine of the rows' gradient.
+ * nvfp4_expert_combine: y[t] = sum over j of w[t,j] * rows[row of (t,j)], summed in fp32 in the order of j; dropped slots add nothing.
+ * nvfp4_expert_combine_bwd: drows[r] = w * dy[token of r's slot] (zero in padding; NULL: not wanted), and
+ *   dweights[t,j] = <dy[t], rows[row of (t,j)]> of weights_dtype, summed in fp32 (0 for a dropped slot).
+ * x, rows, y, dy of `dtype`, 16-byte aligned; cols and ld multiples of 8.
+ */
+NVFP4_API int64_t nvfp4_expert_rows(int64_t tokens, int64_t topk, int64_t experts);
+NVFP4_API int nvfp4_expert_sort(const void* expert_of, int wide, int64_t tokens, int64_t topk, int64_t experts, int32_t* counts,
+                      int32_t* offsets, int32_t* row_of, int32_t* slot_of, void* cuda_stream);
+NVFP4_API int nvfp4_expert_gather(const void* x, int dtype, int64_t tokens, int64_t topk, int64_t experts, int64_t cols, int64_t ld,
+                        const int32_t* offsets, const int32_t* slot_of, const void* weights, int weights_dtype, void* rows,
+                        void* cuda_stream);
+NVFP4_API int nvfp4_expert_combine(const void* rows, int dtype, int64_t tokens, int64_t topk, int64_t experts, int64_t cols,
+                         const int32_t* row_of, const void* weights, int weights_dtype, void* y, void* cuda_stream);
+NVFP4_API int nvfp4_expert_combine_bwd(const void* dy, int dtype, int64_t tokens, int64_t topk, int64_t experts, int64_t cols, int64_t ld,
+                             const int32_t* offsets, const int32_t* slot_of, const int32_t* row_of, const void* rows,
+                             const void* weights, int weights_dtype, void* drows, void* dweights, void* cuda_stream);
+
+/*
+ * The experts' products in FP8, on rows sorted as above; W [experts, N, K].
+ *
+ * nvfp4_quantize_fp8_experts: as nvfp4_quantize_fp8 with block_rows 1 and swizzled scales, of the R sorted rows of x.  by_token == 1: x is
+ *   [tokens, cols] and gathered on the way; 0: x is [R, cols], sorted already.  Either way padding rows count as zero, whatever they
+ *   hold, and rows are multiplied by weights (NULL: 1) before they are quantized.  Blocks along the rows never reach into another
+ *   segment.  Codes of rows that are not used are not written.
+ * nvfp4_gemm_fp8_experts: D[r] = A[r] . B[e]^T for the rows r of segment e; A [rows, K], B [experts, N, K] (codes and scales of the
+ *   matrices one behind the other, as nvfp4_quantize_fp8 leaves a batch), D [rows, N].  rows = R.  For the input gradient B is the transposed
+ *   output of the weights' quantization.
+ * nvfp4_gemm_fp8_experts_dw: D[e] = A[:, segment e] . B[:, segment e]^T: A [N, rows] and B [K, rows], the transposed outputs of the
+ *   rows' quantization, D [experts, N, K] dense.  An expert without rows gets zeros.
+ * nvfp4_experts_fp8_fwd / _bwd: the layer: Y [R, N] from X; dX [R, K] and dW [experts, N, K] from dY, W and X.  x_by_token / dy_by_token and
+ *   dy_weights as by_token and weights above (the weighted sum's output gradient goes in as it is).  N and K multiples of 8, everything
+ *   dense and 16-byte aligned, workspace of nvfp4_experts_fp8_workspace_bytes(..., which) bytes as for nvfp4_linear_fp8_*.
+ */
+NVFP4_API int nvfp4_quantize_fp8_experts(const void* x, int dtype, int by_token, int64_t tokens, int64_t topk, int64_t experts, int64_t cols,
+                               int64_t ld, const int32_t* offsets, const int32_t* slot_of, const void* weights, int weights_dtype,
+                               uint8_t* codes_row, uint8_t* scales_row, uint8_t* codes_t, uint8_t* scales_t, void* cuda_stream);
+NVFP4_API int nvfp4_gemm_fp8_experts(const uint8_t* a_codes, const uint8_t* a_sf, const uint8_t* b_codes, const uint8_t* b_sf,
+                           int64_t experts, const int32_t* offsets, int64_t rows, int64_t N, int64_t K,
+                           void* d, int d_dtype, int64_t ldd, void* cuda_stream);
+NVFP4_API int nvfp4_gemm_fp8_experts_dw(const uint8_t* a_codes, const uint8_t* a_sf, const uint8_t* b_codes, const uint8_t* b_sf,
+                              int64_t experts, const int32_t* offsets, int64_t rows, int64_t N, int64_t K,
+                              void* d, int d_dtype, void* cuda_stream);
+NVFP4_API size_t nvfp4_experts_fp8_workspace_bytes(int64_t tokens, int64_t topk, int64_t experts, int64_t N, int64_t K, int which);
+NVFP4_API int nvfp4_experts_fp8_fwd(const void* X, int x_by_token, const void* W, int dtype, int64_t tokens, int64_t topk, int64_t experts,
+                          int64_t N, int64_t K, const int32_t* offsets, const int32_t* slot_of, void* Y, int y_dtype,
+                          void* workspace, size_t workspace_bytes, void* cuda_stream);
+NVFP4_API int nvfp4_experts_fp8_bwd(const void* dY, int dy_by_token, const void* dy_weights, int weights_dtype, const void* W, const void* X,
+                          int x_by_token, int dtype, int64_t tokens, int64_t topk, int64_t experts, int64_t N, int64_t K,
+                          const int32_t* offsets, const int32_t* slot_of, void* dX, int dx_dtype, void* dW, int dw_dtype,
+                          void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
  * nvfp4_linear_fwd without a caller-supplied workspace and without any device-memory
  * allocation (the paper has no counterpart; this is a library convenience).
  *

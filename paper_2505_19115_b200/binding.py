@@ -104,6 +104,42 @@ def lib():
     L.nvfp4_linear_bwd_bf16_workspace_bytes.argtypes = [i64, i64, i64]
     L.nvfp4_linear_bwd_bf16.restype = ci
     L.nvfp4_linear_bwd_bf16.argtypes = [vp, vp, vp, i64, i64, i64, vp, ci, vp, ci, vp, sz, vp]
+    L.nvfp4_codes_bytes_fp8.restype = sz
+    L.nvfp4_codes_bytes_fp8.argtypes = [i64, i64]
+    L.nvfp4_sf_bytes_fp8.restype = sz
+    L.nvfp4_sf_bytes_fp8.argtypes = [i64, i64, ci]
+    L.nvfp4_linear_fp8_workspace_bytes.restype = sz
+    L.nvfp4_linear_fp8_workspace_bytes.argtypes = [i64, i64, i64, ci]
+    L.nvfp4_expert_rows.restype = i64
+    L.nvfp4_expert_rows.argtypes = [i64, i64, i64]
+    L.nvfp4_experts_fp8_workspace_bytes.restype = sz
+    L.nvfp4_experts_fp8_workspace_bytes.argtypes = [i64, i64, i64, i64, i64, ci]
+    L.nvfp4_quantize_fp8.restype = ci
+    L.nvfp4_quantize_fp8.argtypes = [vp, ci, i64, i64, i64, i64, ci, vp, vp, vp, vp, ci, vp]
+    L.nvfp4_gemm_fp8.restype = ci
+    L.nvfp4_gemm_fp8.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, ci, i64, vp]
+    L.nvfp4_linear_fp8_fwd.restype = ci
+    L.nvfp4_linear_fp8_fwd.argtypes = [vp, vp, ci, i64, i64, i64, vp, ci, vp, sz, vp]
+    L.nvfp4_linear_fp8_bwd.restype = ci
+    L.nvfp4_linear_fp8_bwd.argtypes = [vp, vp, vp, ci, i64, i64, i64, vp, ci, vp, ci, vp, sz, vp]
+    L.nvfp4_expert_sort.restype = ci
+    L.nvfp4_expert_sort.argtypes = [vp, ci, i64, i64, i64, vp, vp, vp, vp, vp]
+    L.nvfp4_expert_gather.restype = ci
+    L.nvfp4_expert_gather.argtypes = [vp, ci, i64, i64, i64, i64, i64, vp, vp, vp, ci, vp, vp]
+    L.nvfp4_expert_combine.restype = ci
+    L.nvfp4_expert_combine.argtypes = [vp, ci, i64, i64, i64, i64, vp, vp, ci, vp, vp]
+    L.nvfp4_expert_combine_bwd.restype = ci
+    L.nvfp4_expert_combine_bwd.argtypes = [vp, ci, i64, i64, i64, i64, i64, vp, vp, vp, vp, vp, ci, vp, vp, vp]
+    L.nvfp4_quantize_fp8_experts.restype = ci
+    L.nvfp4_quantize_fp8_experts.argtypes = [vp, ci, ci, i64, i64, i64, i64, i64, vp, vp, vp, ci, vp, vp, vp, vp, vp]
+    L.nvfp4_gemm_fp8_experts.restype = ci
+    L.nvfp4_gemm_fp8_experts.argtypes = [vp, vp, vp, vp, i64, vp, i64, i64, i64, vp, ci, i64, vp]
+    L.nvfp4_gemm_fp8_experts_dw.restype = ci
+    L.nvfp4_gemm_fp8_experts_dw.argtypes = [vp, vp, vp, vp, i64, vp, i64, i64, i64, vp, ci, vp]
+    L.nvfp4_experts_fp8_fwd.restype = ci
+    L.nvfp4_experts_fp8_fwd.argtypes = [vp, ci, vp, ci, i64, i64, i64, i64, i64, vp, vp, vp, ci, vp, sz, vp]
+    L.nvfp4_experts_fp8_bwd.restype = ci
+    L.nvfp4_experts_fp8_bwd.argtypes = [vp, ci, vp, ci, vp, vp, ci, ci, i64, i64, i64, i64, i64, vp, vp, vp, ci, vp, ci, vp, sz, vp]
     L.nvfp4_linear_fwd_static.restype = ci
     L.nvfp4_linear_fwd_static.argtypes = [vp, vp, ci, i64, i64, i64, ci, vp, vp, rp, rp, vp, ci, vp]
     L.nvfp4_microbench_mma_peak.restype = ci
@@ -483,6 +519,271 @@ def nvfp4_linear_bwd_bf16(dY, W, X, dx_dtype=torch.float32, dw_dtype=torch.float
     dW = torch.empty((N, K), dtype=dw_dtype, device=dY.device)
     ws = _scratch(int(lib().nvfp4_linear_bwd_bf16_workspace_bytes(M, N, K)), dY.device, workspace)
     _check(_native().nvfp4_linear_bwd_bf16(dY, W, X, M, N, K, dX, dX, dW, dW, ws, ws, stream), "nvfp4_linear_bwd_bf16")
+    return dX, dW
+
+
+FP8_FWD, FP8_BWD = 0, 1
+
+
+def nvfp4_codes_bytes_fp8(Rq: int, Kq: int) -> int:
+    return int(lib().nvfp4_codes_bytes_fp8(Rq, Kq))
+
+
+def nvfp4_sf_bytes_fp8(Rq: int, Kq: int, sf_layout: int = SF_SWIZZLED) -> int:
+    return int(lib().nvfp4_sf_bytes_fp8(Rq, Kq, sf_layout))
+
+
+def _fp8_codes(lead, Rq, Kq, device):
+    """Codes [*lead, Rq, Kq], rows of a multiple of 16 bytes."""
+    return torch.empty((*lead, Rq, -(-Kq // 16) * 16), dtype=torch.uint8, device=device)[..., :Kq]
+
+
+def _fp8_outputs(lead, Rq, Kq, sf_layout, device):
+    if sf_layout == SF_LINEAR:
+        return _fp8_codes(lead, Rq, Kq, device), torch.empty((*lead, Rq, -(-Kq // 128)), dtype=torch.uint8, device=device)
+    n = (lead[0] if lead else 1) * (-(-Rq // 128)) * (-(-Kq // 512)) * 512
+    return _fp8_codes(lead, Rq, Kq, device), torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _fp8_operand(codes):
+    """(matrices, Rq, Kq) of codes as the quantizer leaves them."""
+    lead, (Rq, Kq) = codes.shape[:-2], codes.shape[-2:]
+    pitch = -(-Kq // 16) * 16
+    if codes.element_size() != 1 or codes.stride(-1) != 1 or (Rq > 1 and codes.stride(-2) != pitch) or (
+            len(lead) == 1 and lead[0] > 1 and codes.stride(0) != Rq * pitch):
+        raise ValueError("FP8 codes have one byte each and rows of a multiple of 16 bytes, one behind the other")
+    return lead[0] if lead else 1, Rq, Kq
+
+
+def nvfp4_quantize_fp8(x, block_rows: int = 1, row: bool = True, transposed: bool = False, sf_layout: int = SF_SWIZZLED, stream=None):
+    """FP8 with a power-of-two scale for each block of 128 (block_rows 128: 128 x 128, for weights).  x [rows, cols], or dense
+    [batch, rows, cols].  Returns (codes [..., rows, cols], scales, codes_t [..., cols, rows], scales_t), None for what is not wanted;
+    scales: linear [..., Rq, ceil(Kq/128)], or a flat swizzled buffer."""
+    assert x.is_cuda and x.dim() in (2, 3) and x.stride(-1) == 1 and (x.dim() == 2 or x.is_contiguous())
+    lead, (rows, cols) = x.shape[:-2], x.shape[-2:]
+    out = (_fp8_outputs(lead, rows, cols, sf_layout, x.device) if row else (None, None)) + (
+        _fp8_outputs(lead, cols, rows, sf_layout, x.device) if transposed else (None, None))
+    # a matrix of one row has no leading dimension to speak of
+    ld = x.stride(-2) if rows > 1 else max(x.stride(-2), -(-cols // 8) * 8)
+    st = _native().nvfp4_quantize_fp8(x, x, lead[0] if lead else 1, rows, cols, ld, block_rows, *out, sf_layout, stream)
+    _check(st, "nvfp4_quantize_fp8")
+    return out
+
+
+def nvfp4_gemm_fp8(a_codes, a_sf, b_codes, b_sf, out_dtype=torch.float32, out=None, stream=None):
+    """D[M,N] = A[M,K] . B[N,K]^T on FP8 codes with swizzled scales."""
+    (_, M, K), (_, N, Kb) = _fp8_operand(a_codes), _fp8_operand(b_codes)
+    assert K == Kb
+    if out is None:
+        out = torch.empty((M, N), dtype=out_dtype, device=a_codes.device)
+    assert out.shape == (M, N) and out.stride(1) == 1
+    st = _native().nvfp4_gemm_fp8(a_codes, a_sf, b_codes, b_sf, M, N, K, out, out, out.stride(0), stream)
+    _check(st, "nvfp4_gemm_fp8")
+    return out
+
+
+def nvfp4_linear_fp8_workspace_bytes(M: int, N: int, K: int, which: int) -> int:
+    return int(lib().nvfp4_linear_fp8_workspace_bytes(M, N, K, which))
+
+
+def nvfp4_linear_fp8_fwd(X, W, out=None, out_dtype=torch.float32, workspace=None, stream=None):
+    """Y[M,N] = Q(X) . Q(W)^T (Eq. 1) in FP8: blocks of 1 x 128 for X, 128 x 128 for W."""
+    (M, K), N = X.shape, W.shape[0]
+    if out is None:
+        out = torch.empty((M, N), dtype=out_dtype, device=X.device)
+    assert X.is_contiguous() and W.is_contiguous() and out.is_contiguous() and X.dtype == W.dtype and W.shape[1] == K and out.shape == (M, N)
+    if workspace is None:
+        workspace = _scratch(nvfp4_linear_fp8_workspace_bytes(M, N, K, FP8_FWD), X.device, None)
+    st = _native().nvfp4_linear_fp8_fwd(X, W, X, M, N, K, out, out, workspace, workspace, stream)
+    _check(st, "nvfp4_linear_fp8_fwd")
+    return out
+
+
+def nvfp4_linear_fp8_bwd(dY, W, X, dX=None, dW=None, dx_dtype=torch.float32, dw_dtype=torch.float32, workspace=None, stream=None):
+    """dX[M,K] and dW[N,K] (Eq. 2-3) in FP8, every tensor read once.  Returns (dX, dW)."""
+    (M, N), K = dY.shape, W.shape[1]
+    if dX is None:
+        dX = torch.empty((M, K), dtype=dx_dtype, device=dY.device)
+    if dW is None:
+        dW = torch.empty((N, K), dtype=dw_dtype, device=dY.device)
+    assert all(t.is_contiguous() for t in (dY, W, X, dX, dW)) and dY.dtype == W.dtype == X.dtype
+    assert W.shape == dW.shape == (N, K) and X.shape == dX.shape == (M, K)
+    if workspace is None:
+        workspace = _scratch(nvfp4_linear_fp8_workspace_bytes(M, N, K, FP8_BWD), dY.device, None)
+    st = _native().nvfp4_linear_fp8_bwd(dY, W, X, dY, M, N, K, dX, dX, dW, dW, workspace, workspace, stream)
+    _check(st, "nvfp4_linear_fp8_bwd")
+    return dX, dW
+
+
+def nvfp4_expert_rows(tokens: int, topk: int, experts: int) -> int:
+    return int(lib().nvfp4_expert_rows(tokens, topk, experts))
+
+
+class ExpertPlan:
+    """Where the rows of every expert lie (nvfp4_expert_sort): counts [experts], offsets [experts + 1], row_of [tokens, topk] and
+    slot_of [rows], int32 on the device."""
+    __slots__ = ("tokens", "topk", "experts", "rows", "counts", "offsets", "row_of", "slot_of")
+
+    def __init__(self, tokens, topk, experts, device):
+        self.tokens, self.topk, self.experts = tokens, topk, experts
+        self.rows = nvfp4_expert_rows(tokens, topk, experts)
+        if self.rows == 0:
+            raise NvFp4Error(2, "nvfp4_expert_rows")
+        self.counts = torch.empty(experts, dtype=torch.int32, device=device)
+        self.offsets = torch.empty(experts + 1, dtype=torch.int32, device=device)
+        self.row_of = torch.empty((tokens, topk), dtype=torch.int32, device=device)
+        self.slot_of = torch.empty(self.rows, dtype=torch.int32, device=device)
+
+
+def nvfp4_expert_sort(expert_of, experts: int, plan: ExpertPlan = None, stream=None) -> ExpertPlan:
+    """Tokens sorted by expert: expert_of [tokens, topk] (int32 or int64; an index outside [0, experts) drops the slot)."""
+    assert expert_of.is_cuda and expert_of.dim() == 2 and expert_of.is_contiguous()
+    if expert_of.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"unsupported dtype {expert_of.dtype}")
+    tokens, topk = expert_of.shape
+    if plan is None:
+        plan = ExpertPlan(tokens, topk, experts, expert_of.device)
+    assert (plan.tokens, plan.topk, plan.experts) == (tokens, topk, experts)
+    st = _native().nvfp4_expert_sort(expert_of, int(expert_of.dtype == torch.int64), tokens, topk, experts, plan.counts, plan.offsets,
+                                     plan.row_of, plan.slot_of, stream)
+    _check(st, "nvfp4_expert_sort")
+    return plan
+
+
+def _weights(weights, plan):
+    """(tensor or None, its dtype for the call)."""
+    if weights is None:
+        return None, BF16
+    assert weights.is_contiguous() and weights.shape == (plan.tokens, plan.topk)
+    return weights, weights
+
+
+def nvfp4_expert_gather(x, plan, weights=None, out=None, stream=None):
+    """rows[r] = (weight *) x[token of row r], zero in padding; rows that are not used are left as they are."""
+    assert x.dim() == 2 and x.stride(1) == 1 and x.shape[0] == plan.tokens
+    cols = x.shape[1]
+    if out is None:
+        out = torch.empty((plan.rows, cols), dtype=x.dtype, device=x.device)
+    assert out.is_contiguous() and out.shape == (plan.rows, cols) and out.dtype == x.dtype
+    w, w_dtype = _weights(weights, plan)
+    st = _native().nvfp4_expert_gather(x, x, plan.tokens, plan.topk, plan.experts, cols, x.stride(0) if plan.tokens > 1 else cols,
+                                       plan.offsets, plan.slot_of, w, w_dtype, out, stream)
+    _check(st, "nvfp4_expert_gather")
+    return out
+
+
+def nvfp4_expert_combine(rows, plan, weights=None, out=None, stream=None):
+    """y[t] = sum_j (weights[t,j] *) rows[row of (t,j)]; without weights the gradient of nvfp4_expert_gather."""
+    assert rows.is_contiguous() and rows.dim() == 2 and rows.shape[0] == plan.rows
+    cols = rows.shape[1]
+    if out is None:
+        out = torch.empty((plan.tokens, cols), dtype=rows.dtype, device=rows.device)
+    assert out.is_contiguous() and out.shape == (plan.tokens, cols) and out.dtype == rows.dtype
+    w, w_dtype = _weights(weights, plan)
+    st = _native().nvfp4_expert_combine(rows, rows, plan.tokens, plan.topk, plan.experts, cols, plan.row_of, w, w_dtype, out, stream)
+    _check(st, "nvfp4_expert_combine")
+    return out
+
+
+def nvfp4_expert_combine_bwd(dy, rows, plan, weights, rows_gradient: bool = True, drows=None, dweights=None, stream=None):
+    """Gradient of nvfp4_expert_combine by its rows and its weights: (drows, or None where it is not wanted; dweights)."""
+    assert dy.dim() == 2 and dy.stride(1) == 1 and dy.shape[0] == plan.tokens and rows.dtype == dy.dtype
+    cols = dy.shape[1]
+    assert rows.is_contiguous() and rows.shape == (plan.rows, cols)
+    if drows is None and rows_gradient:
+        drows = torch.empty((plan.rows, cols), dtype=rows.dtype, device=rows.device)
+    if dweights is None:
+        dweights = torch.empty_like(weights)
+    assert drows is None or (drows.is_contiguous() and drows.shape == rows.shape and drows.dtype == rows.dtype)
+    assert weights.is_contiguous() and dweights.is_contiguous() and dweights.dtype == weights.dtype
+    assert weights.shape == dweights.shape == (plan.tokens, plan.topk)
+    st = _native().nvfp4_expert_combine_bwd(dy, dy, plan.tokens, plan.topk, plan.experts, cols, dy.stride(0) if plan.tokens > 1 else cols,
+                                            plan.offsets, plan.slot_of, plan.row_of, rows, weights, weights, drows, dweights, stream)
+    _check(st, "nvfp4_expert_combine_bwd")
+    return drows, dweights
+
+
+def _by_token(x, plan, sorted_rows):
+    assert x.dim() == 2 and x.stride(1) == 1 and x.shape[0] == (plan.rows if sorted_rows else plan.tokens)
+    return int(not sorted_rows)
+
+
+def nvfp4_quantize_fp8_experts(x, plan, weights=None, sorted_rows: bool = False, row: bool = True, transposed: bool = False, stream=None):
+    """nvfp4_quantize_fp8 of the sorted rows, gathered on the way from x [tokens, cols] (sorted_rows: x is [rows, cols] already) and
+    multiplied by weights.  Returns (codes [rows, cols], scales, codes_t [cols, rows], scales_t)."""
+    by_token = _by_token(x, plan, sorted_rows)
+    cols = x.shape[1]
+    out = (_fp8_outputs((), plan.rows, cols, SF_SWIZZLED, x.device) if row else (None, None)) + (
+        _fp8_outputs((), cols, plan.rows, SF_SWIZZLED, x.device) if transposed else (None, None))
+    w, w_dtype = _weights(weights, plan)
+    ld = x.stride(0) if x.shape[0] > 1 else max(x.stride(0), -(-cols // 8) * 8)
+    st = _native().nvfp4_quantize_fp8_experts(x, x, by_token, plan.tokens, plan.topk, plan.experts, cols, ld, plan.offsets, plan.slot_of,
+                                              w, w_dtype, *out, stream)
+    _check(st, "nvfp4_quantize_fp8_experts")
+    return out
+
+
+def nvfp4_gemm_fp8_experts(a_codes, a_sf, b_codes, b_sf, plan, out_dtype=torch.float32, out=None, stream=None):
+    """D[r] = A[r] . B[e]^T for the rows r of expert e; A [rows, K], B [experts, N, K]."""
+    (_, R, K), (E, N, Kb) = _fp8_operand(a_codes), _fp8_operand(b_codes)
+    assert K == Kb and R == plan.rows and E == plan.experts
+    if out is None:
+        out = torch.empty((R, N), dtype=out_dtype, device=a_codes.device)
+    assert out.shape == (R, N) and out.stride(1) == 1
+    st = _native().nvfp4_gemm_fp8_experts(a_codes, a_sf, b_codes, b_sf, E, plan.offsets, R, N, K, out, out, out.stride(0), stream)
+    _check(st, "nvfp4_gemm_fp8_experts")
+    return out
+
+
+def nvfp4_gemm_fp8_experts_dw(a_codes, a_sf, b_codes, b_sf, plan, out_dtype=torch.float32, out=None, stream=None):
+    """D[e] = A[:, rows of e] . B[:, rows of e]^T; A [N, rows], B [K, rows] (transposed outputs of nvfp4_quantize_fp8_experts)."""
+    (_, N, R), (_, K, Rb) = _fp8_operand(a_codes), _fp8_operand(b_codes)
+    assert R == Rb == plan.rows
+    if out is None:
+        out = torch.empty((plan.experts, N, K), dtype=out_dtype, device=a_codes.device)
+    assert out.shape == (plan.experts, N, K) and out.is_contiguous()
+    st = _native().nvfp4_gemm_fp8_experts_dw(a_codes, a_sf, b_codes, b_sf, plan.experts, plan.offsets, R, N, K, out, out, stream)
+    _check(st, "nvfp4_gemm_fp8_experts_dw")
+    return out
+
+
+def nvfp4_experts_fp8_workspace_bytes(tokens: int, topk: int, experts: int, N: int, K: int, which: int) -> int:
+    return int(lib().nvfp4_experts_fp8_workspace_bytes(tokens, topk, experts, N, K, which))
+
+
+def nvfp4_experts_fp8_fwd(X, W, plan, sorted_rows: bool = False, out=None, out_dtype=None, workspace=None, stream=None):
+    """Y[r] = Q(X[r]) . Q(W[e])^T for the rows r of expert e, W [experts, N, K]; X [tokens, K] is gathered on the way (sorted_rows:
+    X is [rows, K] already).  Y [rows, N] of X's dtype unless told otherwise."""
+    by_token, (E, N, K) = _by_token(X, plan, sorted_rows), W.shape
+    if out is None:
+        out = torch.empty((plan.rows, N), dtype=out_dtype or X.dtype, device=X.device)
+    assert X.is_contiguous() and W.is_contiguous() and out.is_contiguous() and X.dtype == W.dtype and X.shape[1] == K
+    assert E == plan.experts and out.shape == (plan.rows, N)
+    if workspace is None:
+        workspace = _scratch(nvfp4_experts_fp8_workspace_bytes(plan.tokens, plan.topk, E, N, K, FP8_FWD), X.device, None)
+    st = _native().nvfp4_experts_fp8_fwd(X, by_token, W, X, plan.tokens, plan.topk, E, N, K, plan.offsets, plan.slot_of, out, out,
+                                         workspace, workspace, stream)
+    _check(st, "nvfp4_experts_fp8_fwd")
+    return out
+
+
+def nvfp4_experts_fp8_bwd(dY, W, X, plan, weights=None, dy_sorted_rows: bool = False, sorted_rows: bool = False, dX=None, dW=None,
+                          dx_dtype=None, dw_dtype=torch.float32, workspace=None, stream=None):
+    """dX [rows, K] and dW [experts, N, K].  dY [tokens, N] is gathered on the way and multiplied by weights, as the gradient of
+    nvfp4_expert_combine (dy_sorted_rows: dY is [rows, N] already); X as in nvfp4_experts_fp8_fwd.  Returns (dX, dW)."""
+    dy_by_token, x_by_token, (E, N, K) = _by_token(dY, plan, dy_sorted_rows), _by_token(X, plan, sorted_rows), W.shape
+    if dX is None:
+        dX = torch.empty((plan.rows, K), dtype=dx_dtype or X.dtype, device=dY.device)
+    if dW is None:
+        dW = torch.empty((E, N, K), dtype=dw_dtype, device=dY.device)
+    assert all(t.is_contiguous() for t in (dY, W, X, dX, dW)) and dY.dtype == W.dtype == X.dtype
+    assert E == plan.experts and dY.shape[1] == N and X.shape[1] == K and dX.shape == (plan.rows, K) and dW.shape == W.shape
+    w, w_dtype = _weights(weights, plan)
+    if workspace is None:
+        workspace = _scratch(nvfp4_experts_fp8_workspace_bytes(plan.tokens, plan.topk, E, N, K, FP8_BWD), dY.device, None)
+    st = _native().nvfp4_experts_fp8_bwd(dY, dy_by_token, w, w_dtype, W, X, x_by_token, dY, plan.tokens, plan.topk, E, N, K, plan.offsets,
+                                         plan.slot_of, dX, dX, dW, dW, workspace, workspace, stream)
+    _check(st, "nvfp4_experts_fp8_bwd")
     return dX, dW
 
 

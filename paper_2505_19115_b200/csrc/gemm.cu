@@ -20,6 +20,7 @@
 #include <type_traits>
 
 #include "bounded_waits.cuh"
+#include "fp8.cuh"
 #include "quantize_core.cuh"
 #include "tc_ptx.cuh"
 #include "tensor_map.cuh"
@@ -1325,6 +1326,8 @@ extern "C" int nvfp4_device_error_word(uint32_t* host_out) {
   if (w != 0 && cudaMemcpyToSymbol(g_error_word, &zero, sizeof(zero)) != cudaSuccess) return NVFP4_ERR_CUDA;
   unsigned int tile_w = 0;
   if (int st = tile_error_word(&tile_w)) return st;
+  w |= tile_w;
+  if (int st = fp8_error_word(&tile_w)) return st;
   w |= tile_w;
   *host_out = w;
   return NVFP4_OK;

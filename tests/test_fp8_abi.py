@@ -1,0 +1,128 @@
+"""FP8 and expert entry points: sizes, and arguments refused on the host before any launch (no GPU needed)."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2505_19115_b200 import binding as nb
+
+P, ODD = 0x1000, 0x1004           # never dereferenced: every call below fails validation first
+BIG = 1 << 40
+
+
+def test_sizes():
+    assert nb.nvfp4_codes_bytes_fp8(3, 17) == 96 and nb.nvfp4_codes_bytes_fp8(0, 17) == 0
+    assert nb.nvfp4_sf_bytes_fp8(3, 129, nb.SF_LINEAR) == 6
+    assert nb.nvfp4_sf_bytes_fp8(129, 513, nb.SF_SWIZZLED) == 2 * 2 * 512
+    assert nb.nvfp4_sf_bytes_fp8(129, 513, 2) == 0 and nb.nvfp4_sf_bytes_fp8(-1, 5, 0) == 0
+    for which in (nb.FP8_FWD, nb.FP8_BWD):
+        assert nb.nvfp4_linear_fp8_workspace_bytes(1, 512, 512, which) % 256 == 0 < nb.nvfp4_linear_fp8_workspace_bytes(1, 512, 512, which)
+        assert nb.nvfp4_linear_fp8_workspace_bytes(16, 500, 512, which) == 0 == nb.nvfp4_linear_fp8_workspace_bytes(0, 512, 512, which)
+        assert nb.nvfp4_experts_fp8_workspace_bytes(16, 2, 8, 64, 64, which) > 0 == nb.nvfp4_experts_fp8_workspace_bytes(16, 2, 1025, 64, 64, which)
+    assert nb.nvfp4_linear_fp8_workspace_bytes(16, 512, 512, 2) == 0
+
+
+@pytest.mark.parametrize("size,rows", [((1, 1, 1), 128), ((1, 8, 64), 1024), ((1, 8, 4), 512), ((100, 2, 3), 512), ((128, 1, 1), 128), ((129, 1, 1), 256)])
+def test_expert_rows_hold_any_distribution(size, rows):
+    T, k, E = size
+    assert nb.nvfp4_expert_rows(T, k, E) == rows
+    n = T * k
+    spread = [n // min(n, E) + (i < n % min(n, E)) for i in range(min(n, E))]
+    worst = [1] * (min(n, E) - 1) + [n - min(n, E) + 1]
+    for counts in (spread, worst, [n]):
+        assert sum(-(-c // 128) * 128 for c in counts) <= rows
+
+
+def test_expert_rows_refuse():
+    for bad in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (1, 1, 1025), (1 << 31, 1, 1), (1 << 30, 1 << 30, 8), (-1, 2, 2)):
+        assert nb.nvfp4_expert_rows(*bad) == 0
+
+
+def _call(name, defaults, status, **changes):
+    args = [changes.get(k, v) for k, v in defaults.items()]
+    assert set(changes) <= set(defaults)
+    got = getattr(nb.lib(), name)(*[C.c_void_p(a) if isinstance(a, int) and k in POINTERS else a for (k, _), a in zip(defaults.items(), args)])
+    assert got == status, (name, changes, got)
+
+
+POINTERS = {"x", "cr", "sr", "ct", "st", "a", "asf", "b", "bsf", "d", "X", "W", "Y", "dY", "dX", "dW", "ws", "offsets", "slot", "row", "w", "rows", "y", "dy",
+            "drows", "dw", "e", "counts", "stream"}
+
+
+def test_quantizer_refusals():
+    q = dict(x=P, dtype=0, batch=1, rows_=16, cols=32, ld=32, block=1, cr=P, sr=P, ct=P, st=P, layout=1, stream=None)
+    for status, changes in ((1, dict(x=None)), (1, dict(cr=None)), (1, dict(st=None)), (1, dict(cr=None, sr=None, ct=None, st=None)), (4, dict(dtype=2)),
+                            (4, dict(layout=2)), (4, dict(block=64)), (2, dict(batch=0)), (2, dict(rows_=0)), (2, dict(cols=-1)), (2, dict(ld=24)),
+                            (2, dict(rows_=1 << 33)), (2, dict(batch=1 << 20, rows_=1 << 20, cols=1 << 20, ld=1 << 20)), (3, dict(x=ODD)), (3, dict(ld=36)),
+                            (3, dict(cr=ODD)), (3, dict(st=ODD))):
+        _call("nvfp4_quantize_fp8", q, status, **changes)
+
+
+def test_product_refusals():
+    g = dict(a=P, asf=P, b=P, bsf=P, M=1, N=8, K=100, d=P, dtype=1, ldd=8, stream=None)
+    for status, changes in ((1, dict(a=None)), (1, dict(bsf=None)), (1, dict(d=None)), (4, dict(dtype=7)), (2, dict(M=0)), (2, dict(K=0)), (2, dict(ldd=4)),
+                            (2, dict(M=BIG)), (2, dict(M=1 << 30, N=1 << 30, ldd=1 << 30)), (3, dict(a=ODD)), (3, dict(d=ODD)), (3, dict(ldd=10)), (3, dict(dtype=0, ldd=12))):
+        _call("nvfp4_gemm_fp8", g, status, **changes)
+    g = dict(a=P, asf=P, b=P, bsf=P, E=4, offsets=P, rows_=256, N=8, K=100, d=P, dtype=1, ldd=8, stream=None)
+    for status, changes in ((1, dict(a=None)), (1, dict(offsets=None)), (4, dict(dtype=7)), (2, dict(E=0)), (2, dict(E=1025)), (2, dict(rows_=200)), (2, dict(rows_=0)),
+                            (2, dict(E=1024, N=1 << 22, ldd=1 << 22)), (3, dict(offsets=0x1002)), (3, dict(ldd=9))):
+        _call("nvfp4_gemm_fp8_experts", g, status, **changes)
+    g = dict(a=P, asf=P, b=P, bsf=P, E=4, offsets=P, rows_=256, N=8, K=104, d=P, dtype=1, stream=None)
+    for status, changes in ((1, dict(b=None)), (1, dict(offsets=None)), (4, dict(dtype=7)), (2, dict(E=1025)), (2, dict(rows_=200)), (2, dict(N=0)), (3, dict(K=102)), (3, dict(d=ODD))):
+        _call("nvfp4_gemm_fp8_experts_dw", g, status, **changes)
+
+
+def test_layer_refusals():
+    f = dict(X=P, W=P, dtype=0, M=7, N=64, K=64, Y=P, ydtype=1, ws=P, wsb=1 << 30, stream=None)
+    for status, changes in ((1, dict(X=None)), (1, dict(Y=None)), (4, dict(dtype=5)), (4, dict(ydtype=5)), (2, dict(M=0)), (2, dict(N=60)), (2, dict(K=4)), (2, dict(M=BIG)),
+                            (3, dict(W=ODD)), (3, dict(Y=ODD)), (5, dict(ws=None)), (5, dict(wsb=100)), (5, dict(ws=0x1010))):
+        _call("nvfp4_linear_fp8_fwd", f, status, **changes)
+    b = dict(dY=P, W=P, X=P, dtype=0, M=7, N=64, K=64, dX=P, dxdtype=1, dW=P, dwdtype=1, ws=P, wsb=1 << 30, stream=None)
+    for status, changes in ((1, dict(dY=None)), (1, dict(dW=None)), (4, dict(dxdtype=5)), (4, dict(dwdtype=-1)), (2, dict(N=63)), (3, dict(dX=ODD)), (5, dict(ws=None)), (5, dict(wsb=0))):
+        _call("nvfp4_linear_fp8_bwd", b, status, **changes)
+
+
+def test_routing_refusals():
+    s = dict(e=P, wide=0, T=4, k=2, E=8, counts=P, offsets=P, row=P, slot=P, stream=None)
+    for status, changes in ((1, dict(e=None)), (1, dict(slot=None)), (4, dict(wide=2)), (2, dict(T=0)), (2, dict(E=1025)), (2, dict(k=0)), (3, dict(e=0x1002)), (3, dict(e=ODD, wide=1)),
+                            (3, dict(row=0x1001))):
+        _call("nvfp4_expert_sort", s, status, **changes)
+    g = dict(x=P, dtype=0, T=4, k=2, E=8, cols=64, ld=64, offsets=P, slot=P, w=P, wdtype=1, rows=P, stream=None)
+    for status, changes in ((1, dict(x=None)), (1, dict(offsets=None)), (4, dict(dtype=3)), (4, dict(wdtype=3)), (2, dict(cols=60)), (2, dict(ld=56)), (2, dict(T=0)), (3, dict(x=ODD)),
+                            (3, dict(ld=68)), (3, dict(w=0x1002)), (3, dict(rows=ODD))):
+        _call("nvfp4_expert_gather", g, status, **changes)
+    c = dict(rows=P, dtype=0, T=4, k=2, E=8, cols=64, row=P, w=P, wdtype=0, y=P, stream=None)
+    for status, changes in ((1, dict(rows=None)), (1, dict(row=None)), (4, dict(dtype=3)), (2, dict(cols=0)), (2, dict(E=0)), (3, dict(y=ODD)), (3, dict(w=0x1001))):
+        _call("nvfp4_expert_combine", c, status, **changes)
+    b = dict(dy=P, dtype=0, T=4, k=2, E=8, cols=64, ld=64, offsets=P, slot=P, row=P, rows=P, w=P, wdtype=1, drows=None, dw=P, stream=None)
+    for status, changes in ((1, dict(dy=None)), (1, dict(w=None)), (1, dict(dw=None)), (4, dict(wdtype=9)), (2, dict(cols=12)), (2, dict(k=-1)), (3, dict(drows=ODD)), (3, dict(dw=0x1002))):
+        _call("nvfp4_expert_combine_bwd", b, status, **changes)
+
+
+def test_experts_refusals():
+    q = dict(x=P, dtype=0, by=1, T=4, k=2, E=8, cols=60, ld=64, offsets=P, slot=P, w=None, wdtype=0, cr=P, sr=P, ct=None, st=None, stream=None)
+    for status, changes in ((1, dict(x=None)), (1, dict(cr=None)), (1, dict(slot=None)), (4, dict(by=2)), (4, dict(wdtype=4)), (2, dict(ld=56)), (2, dict(T=0)), (3, dict(x=ODD)), (3, dict(ld=60)),
+                            (3, dict(w=0x1001)), (3, dict(sr=ODD))):
+        _call("nvfp4_quantize_fp8_experts", q, status, **changes)
+    f = dict(X=P, by=1, W=P, dtype=0, T=4, k=2, E=8, N=64, K=64, offsets=P, slot=P, Y=P, ydtype=0, ws=P, wsb=1 << 30, stream=None)
+    for status, changes in ((1, dict(W=None)), (1, dict(offsets=None)), (4, dict(by=-1)), (4, dict(ydtype=2)), (2, dict(N=60)), (2, dict(E=1025)), (2, dict(T=0)), (3, dict(Y=ODD)), (3, dict(slot=0x1001)),
+                            (5, dict(ws=None)), (5, dict(wsb=1))):
+        _call("nvfp4_experts_fp8_fwd", f, status, **changes)
+    b = dict(dY=P, by=1, w=None, wdtype=0, W=P, X=P, xby=1, dtype=0, T=4, k=2, E=8, N=64, K=64, offsets=P, slot=P, dX=P, dxdtype=0, dW=P, dwdtype=1, ws=P, wsb=1 << 30, stream=None)
+    for status, changes in ((1, dict(dY=None)), (1, dict(dX=None)), (4, dict(xby=2)), (4, dict(wdtype=2)), (2, dict(K=60)), (3, dict(dW=ODD)), (3, dict(w=0x1001)), (5, dict(ws=0x1001))):
+        _call("nvfp4_experts_fp8_bwd", b, status, **changes)
+
+
+def test_codes_that_are_not_laid_out_as_the_quantizer_leaves_them_are_refused():
+    good = torch.zeros((4, 32), dtype=torch.uint8)
+    sf = torch.zeros(512, dtype=torch.uint8)
+    for bad in (torch.zeros((4, 24), dtype=torch.uint8), torch.zeros((4, 64), dtype=torch.uint8)[:, :32], good.T, torch.zeros((4, 32), dtype=torch.int16)):
+        with pytest.raises(ValueError):
+            nb.nvfp4_gemm_fp8(bad, sf, good, sf, out=torch.zeros((4, 4)))
+
+
+def test_expert_choices_are_whole_numbers():
+    class OnDevice(torch.Tensor):
+        is_cuda = True
+    with pytest.raises(TypeError):
+        nb.nvfp4_expert_sort(torch.zeros((2, 2)).as_subclass(OnDevice), 4)
