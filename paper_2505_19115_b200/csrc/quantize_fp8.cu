@@ -6,7 +6,11 @@
 // which is one block of 128 for every row and every column, so no scale needs a second read.  A thread holds 8 rows x 8
 // columns in registers (eight 16-byte loads in flight): a row's maximum is a reduction over 16 lanes, a column's one over the
 // thread's own rows and then, through shared memory, over the warps.  Row codes leave from registers, 128 bytes of a row per
-// half warp; transposed ones are packed along the thread's 8 rows and turned round in shared memory.
+// half warp; transposed ones are packed along the thread's 8 rows and turned round in shared memory.  Nothing behind the last row or
+// column is written.
+// 8192 x 8192 bf16 (buffers in turn, nothing in the caches): row output 31 us = 6.5 TB/s, transposed 35 = 5.7, both 48 = 5.6; 16384 x
+// 11008 78 / 89 / 123 us = 6.9 / 6.1 / 5.9; fp32 8192 x 8192 50 / 53 / 70.  (A copy: 6.3-6.5 TB/s.)  With a branch around each load,
+// 64-bit tile indices and a shuffled maximum per row the kernel was bound by instruction issue (18.6 per element): both 74 us.
 #include <cuda_bf16.h>
 
 #include <type_traits>
@@ -21,9 +25,8 @@ struct Fp8Op {
   Fp8Operand o;
   int64_t pitch_r, pitch_t;
   int64_t sf_r, sf_t;            // bytes of one matrix's scales
-  int64_t nb_r, nb_t;            // blocks per quantized row
-  int64_t col_tiles, row_tiles;
-  int64_t first;                 // first tile of the launch that belongs to it
+  int col_tiles, row_tiles;      // = blocks per quantized row of codes_r, codes_t
+  int first;                     // first tile of the launch that belongs to it
 };
 struct Fp8Ops {
   Fp8Op op[kMaxFp8Operands];
@@ -33,111 +36,149 @@ struct Fp8Ops {
 __device__ __forceinline__ uint32_t absmax_nan_bf16x2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r & 0x7FFF7FFFu;
+  return r;                                            // the sign bits mean nothing
 }
 
 __device__ __forceinline__ float load_weight(const void* w, int dtype, int64_t i) {
-  if (dtype == NVFP4_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(w)[i]);
-  return static_cast<const float*>(w)[i];
+  if (dtype == NVFP4_BF16) return __uint_as_float((uint32_t)reinterpret_cast<const volatile uint16_t*>(w)[i] << 16);
+  return reinterpret_cast<const volatile float*>(w)[i];
 }
 
-// A thread's 8 x 8 values.  bf16 stays packed, unless it is multiplied by a weight.
+// A thread's 8 x 8 values; bf16 stays packed.  A row's weight is multiplied in where a value is used (one rounding in fp32).
 template <typename T, bool WEIGHTED>
 struct Values {
-  static constexpr bool kPacked = std::is_same_v<T, __nv_bfloat16> && !WEIGHTED;
+  static constexpr bool kPacked = std::is_same_v<T, __nv_bfloat16>;
   static constexpr int kWords = kPacked ? 4 : 8;
   uint32_t raw[8][kWords];
+  float weight[WEIGHTED ? 8 : 1];
 
   __device__ __forceinline__ float get(int i, int j) const {
-    if constexpr (kPacked) return __uint_as_float((j & 1) ? raw[i][j >> 1] & 0xFFFF0000u : raw[i][j >> 1] << 16);
-    else return __uint_as_float(raw[i][j]);
+    float v;
+    if constexpr (kPacked) v = __uint_as_float((j & 1) ? raw[i][j >> 1] & 0xFFFF0000u : raw[i][j >> 1] << 16);
+    else v = __uint_as_float(raw[i][j]);
+    if constexpr (WEIGHTED) v = __fmul_rn(v, weight[i]);
+    return v;
   }
-  // The row's 8 values from `src` (null: zeros), of which `left` exist.
-  __device__ __forceinline__ void load(int i, const T* src, int left, [[maybe_unused]] float weight) {
-    uint32_t w[8];
-    constexpr int kSource = std::is_same_v<T, __nv_bfloat16> ? 4 : 8;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) w[q] = 0u;
-    if (src && left >= 8) {
-      const uint4 a = load_vec16(src);
-      w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-      if constexpr (kSource == 8) {
-        const uint4 b = load_vec16(src + 4);
-        w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
-      }
-    } else if (src) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (j >= left) break;
-        if constexpr (kSource == 8) w[j] = reinterpret_cast<const volatile uint32_t*>(src)[j];
-        else w[j >> 1] |= (uint32_t)reinterpret_cast<const volatile uint16_t*>(src)[j] << (16 * (j & 1));
-      }
-    }
-#pragma unroll
-    for (int q = 0; q < kWords; ++q) {
-      if constexpr (kPacked || !WEIGHTED) raw[i][q] = w[q];
-      else if constexpr (kSource == 8) raw[i][q] = __float_as_uint(__fmul_rn(__uint_as_float(w[q]), weight));
-      else raw[i][q] = __float_as_uint(__fmul_rn(__uint_as_float((q & 1) ? w[q >> 1] & 0xFFFF0000u : w[q >> 1] << 16), weight));
+  // Row i, all 8 values of it.
+  __device__ __forceinline__ void load(int i, const T* src) {
+    const uint4 a = load_vec16(src);
+    raw[i][0] = a.x; raw[i][1] = a.y; raw[i][2] = a.z; raw[i][3] = a.w;
+    if constexpr (!kPacked) {
+      const uint4 b = load_vec16(src + 4);
+      raw[i][4] = b.x; raw[i][5] = b.y; raw[i][6] = b.z; raw[i][7] = b.w;
     }
   }
-  // Bits of the largest |value| of row i, and of every column.
+  __device__ __forceinline__ void clear(int i) {
+#pragma unroll
+    for (int q = 0; q < kWords; ++q) raw[i][q] = 0u;
+  }
+  // The first `left` values of row i.
+  __device__ __forceinline__ void load_some(int i, const T* src, int left) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (j >= left) break;
+      if constexpr (kPacked) raw[i][j >> 1] |= (uint32_t)reinterpret_cast<const volatile uint16_t*>(src)[j] << (16 * (j & 1));
+      else raw[i][j] = reinterpret_cast<const volatile uint32_t*>(src)[j];
+    }
+  }
+  // Bits of the largest |value| of row i (rounding is monotone: the largest product is that of the largest value), and of every column.
   __device__ __forceinline__ uint32_t row_max(int i) const {
+    uint32_t m = 0u;
     if constexpr (kPacked) {
-      const uint32_t m = absmax_nan_bf16x2(absmax_nan_bf16x2(raw[i][0], raw[i][1]), absmax_nan_bf16x2(raw[i][2], raw[i][3]));
-      return max(m & 0xFFFFu, m >> 16) << 16;
+      const uint32_t p = absmax_nan_bf16x2(absmax_nan_bf16x2(raw[i][0], raw[i][1]), absmax_nan_bf16x2(raw[i][2], raw[i][3]));
+      m = max(p & 0x7FFFu, (p >> 16) & 0x7FFFu) << 16;
     } else {
-      uint32_t m = 0u;
 #pragma unroll
       for (int j = 0; j < 8; ++j) m = max(m, raw[i][j] & 0x7FFFFFFFu);
-      return m;
     }
+    if constexpr (WEIGHTED) m = __float_as_uint(__fmul_rn(__uint_as_float(m), weight[i])) & 0x7FFFFFFFu;
+    return m;
   }
   __device__ __forceinline__ void col_max(uint32_t (&m)[8]) const {
+    if constexpr (kPacked && !WEIGHTED) {
 #pragma unroll
-    for (int j = 0; j < kWords; ++j) {
-      uint32_t v = raw[0][j];
-      if constexpr (!kPacked) v &= 0x7FFFFFFFu;
+      for (int j = 0; j < 4; ++j) {
+        uint32_t v = raw[0][j];
 #pragma unroll
-      for (int i = 1; i < 8; ++i) {
-        if constexpr (kPacked) v = absmax_nan_bf16x2(v, raw[i][j]);
-        else v = max(v, raw[i][j] & 0x7FFFFFFFu);
+        for (int i = 1; i < 8; ++i) v = absmax_nan_bf16x2(v, raw[i][j]);
+        m[2 * j] = (v & 0x7FFFu) << 16; m[2 * j + 1] = v & 0x7FFF0000u;
       }
-      if constexpr (kPacked) { m[2 * j] = v << 16; m[2 * j + 1] = v & 0xFFFF0000u; }
-      else m[j] = v;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        m[j] = 0u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m[j] = max(m[j], __float_as_uint(get(i, j)) & 0x7FFFFFFFu);
+      }
     }
   }
 };
 
-// Byte of the scale of (row r, block kb) of one quantized matrix.
-__device__ __forceinline__ int64_t scale_at(int64_t r, int64_t kb, int64_t nb, int swizzled) {
-  return swizzled ? sf_swizzled_offset(r, kb, (nb + 3) >> 2) : r * nb + kb;
-}
-// The scale of row r (of `rows`) in block kb, written by the thread that has it; tiles hold zero where there is no row or block.
-__device__ __forceinline__ void store_scale(uint8_t* sf, int64_t r, int64_t rows, int64_t kb, int64_t nb, int swizzled, uint32_t code) {
+// The scale of row r (of `rows`) in block kb (of nb), written by the thread that has it; tiles hold zero where there is no row or block.
+__device__ __forceinline__ void store_scale(uint8_t* sf, int64_t r, int64_t rows, int kb, int nb, int swizzled, uint32_t code) {
   if (!swizzled) {
     if (r < rows) sf[r * nb + kb] = (uint8_t)code;
     return;
   }
-  sf[scale_at(r, kb, nb, 1)] = r < rows ? (uint8_t)code : (uint8_t)0;
+  uint8_t* const at = sf + sf_swizzled_offset(r, kb, (nb + 3) >> 2);
+  *at = r < rows ? (uint8_t)code : (uint8_t)0;
   if (kb == nb - 1)
-    for (int64_t p = nb; p & 3; ++p) sf[scale_at(r, p, nb, 1)] = 0;
+    for (int q = 1; (kb + q) & 3; ++q) at[q] = 0;
+}
+
+// Four values scaled, as codes.
+__device__ __forceinline__ uint32_t scaled_codes(float v0, float v1, float v2, float v3, float inv) {
+  float y0, y1, y2, y3;
+  mul2(v0, v1, inv, y0, y1);
+  mul2(v2, v3, inv, y2, y3);
+  return e4m3x4(y0, y1, y2, y3);
+}
+
+// Of the `n` bytes at dst that are to be written, up to 8.
+__device__ __forceinline__ void store_codes(uint8_t* dst, int n, uint32_t lo, uint32_t hi) {
+  if (n >= 8) {
+    *reinterpret_cast<uint2*>(dst) = make_uint2(lo, hi);
+  } else {
+    for (int q = 0; q < n; ++q) dst[q] = (uint8_t)((q < 4 ? lo : hi) >> (8 * (q & 3)));
+  }
+}
+
+// The maxima of a thread's 8 rows -> the one of row l16 / 2 over all 16 lanes.  Each step hands half of the rows to the other lane
+// of a pair, so that 8 + 1 exchanges (5 on packed halves) do what 32 would, and a row's scale is computed by one lane pair, not by all.
+__device__ __forceinline__ uint32_t own_row_max(const uint32_t (&m)[8], int l16) {
+  uint32_t a[4], b[2], c;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {                          // lanes 8-15 keep rows 4-7
+    const bool up = l16 & 8;
+    const uint32_t keep = up ? m[q + 4] : m[q], give = up ? m[q] : m[q + 4];
+    a[q] = max(keep, __shfl_xor_sync(0xFFFFFFFFu, give, 8));
+  }
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const bool up = l16 & 4;
+    const uint32_t keep = up ? a[q + 2] : a[q], give = up ? a[q] : a[q + 2];
+    b[q] = max(keep, __shfl_xor_sync(0xFFFFFFFFu, give, 4));
+  }
+  const bool up = l16 & 2;
+  c = max(up ? b[1] : b[0], __shfl_xor_sync(0xFFFFFFFFu, up ? b[0] : b[1], 2));
+  return max(c, __shfl_xor_sync(0xFFFFFFFFu, c, 1));
 }
 
 template <typename T, bool WEIGHTED>
-__global__ void __launch_bounds__(256) quantize_fp8_kernel(const __grid_constant__ Fp8Ops ops) {
+__global__ void __launch_bounds__(256, std::is_same_v<T, __nv_bfloat16> ? WEIGHTED ? 3 : 4 : 2) quantize_fp8_kernel(const __grid_constant__ Fp8Ops ops) {
   __shared__ __align__(16) uint8_t turned[128 * 128];
-  __shared__ uint32_t col_bits[8][128];
-  __shared__ float col_inverse[128];
+  __shared__ __align__(16) uint32_t col_bits[8][128];
+  __shared__ __align__(16) float col_inverse[128];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15;
   int w = 0;
-  while (w + 1 < ops.n && (int64_t)blockIdx.x >= ops.op[w + 1].first) ++w;
+  while (w + 1 < ops.n && (int)blockIdx.x >= ops.op[w + 1].first) ++w;
   const Fp8Op& op = ops.op[w];
   const Fp8Operand& o = op.o;
-  int64_t tile = (int64_t)blockIdx.x - op.first;
-  const int64_t per_matrix = op.col_tiles * op.row_tiles, b = tile / per_matrix;
-  tile -= b * per_matrix;
-  const int64_t rt = tile / op.col_tiles, ct = tile - rt * op.col_tiles;
-  const int64_t r0 = rt * 128, c0 = ct * 128;
+  int rt = ((int)blockIdx.x - op.first) / op.col_tiles;
+  const int ct = (int)blockIdx.x - op.first - rt * op.col_tiles;
+  const int b = o.batch == 1 ? 0 : rt / op.row_tiles;
+  rt -= b * op.row_tiles;
+  const int64_t r0 = (int64_t)rt * 128, c0 = (int64_t)ct * 128;
   const int64_t row = r0 + warp * 16 + half * 8, col = c0 + l16 * 8;      // of this thread's first value
 
   grid_dependency_wait();
@@ -145,36 +186,52 @@ __global__ void __launch_bounds__(256) quantize_fp8_kernel(const __grid_constant
   if (o.from.used && r0 >= *reinterpret_cast<const volatile int32_t*>(o.from.used)) return;
 
   Values<T, WEIGHTED> v;
-  const T* const x = static_cast<const T*>(o.x) + b * o.rows * o.ld;
+  const T* const x = static_cast<const T*>(o.x) + b * o.rows * o.ld + col;
   const int left = (int)min((int64_t)8, o.cols - col);
-  if (o.from.slot_of) {
-    int slot[8];
+  if constexpr (WEIGHTED) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v.weight[i] = 1.0f;
+  }
+  if (o.from.slot_of) {                                  // rows: a multiple of 128
+    // lane i of a half warp finds row i's source
+    int slot = reinterpret_cast<const volatile int32_t*>(o.from.slot_of)[row + (l16 & 7)];
+    if (slot >= o.from.slots) slot = -1;
+    const int source = slot < 0 ? -1 : o.from.per_row ? slot / o.from.per_row : (int)row + (l16 & 7);
+    float weight = 1.0f;
+    if constexpr (WEIGHTED)
+      if (o.from.weights && slot >= 0) weight = load_weight(o.from.weights, o.from.weights_dtype, slot);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      slot[i] = reinterpret_cast<const volatile int32_t*>(o.from.slot_of)[row + i];   // rows: a multiple of 128
-      if (slot[i] >= o.from.slots) slot[i] = -1;
+      const int from = __shfl_sync(0xFFFFFFFFu, source, i, 16);
+      if constexpr (WEIGHTED) v.weight[i] = __shfl_sync(0xFFFFFFFFu, weight, i, 16);
+      if (left == 8) v.load(i, x + (int64_t)max(from, 0) * o.ld);
+      else {
+        v.clear(i);
+        if (from >= 0) v.load_some(i, x + (int64_t)from * o.ld, left);
+      }
     }
+    if (__any_sync(0xFFFFFFFFu, source < 0)) {           // padding: loaded from row 0 so that no load waits for a branch
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float weight = 1.0f;
-      if (WEIGHTED && o.from.weights && slot[i] >= 0) weight = load_weight(o.from.weights, o.from.weights_dtype, slot[i]);
-      const int64_t source = o.from.per_row ? slot[i] / o.from.per_row : row + i;
-      v.load(i, slot[i] >= 0 && left > 0 ? x + source * o.ld + col : nullptr, left, weight);
+      for (int i = 0; i < 8; ++i)
+        if (__shfl_sync(0xFFFFFFFFu, source, i, 16) < 0) v.clear(i);
     }
+  } else if (r0 + 128 <= o.rows && c0 + 128 <= o.cols) {   // a whole tile: eight loads in flight
+    const T* src = x + row * o.ld;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v.load(i, src + i * o.ld);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v.load(i, row + i < o.rows && left > 0 ? x + (row + i) * o.ld + col : nullptr, left, 1.0f);
+    for (int i = 0; i < 8; ++i) {
+      v.clear(i);
+      if (row + i < o.rows && left == 8) v.load(i, x + (row + i) * o.ld);
+      else if (row + i < o.rows && left > 0) v.load_some(i, x + (row + i) * o.ld, left);
+    }
   }
 
-  uint8_t* const codes_r = o.codes_r ? o.codes_r + (b * o.rows) * op.pitch_r : nullptr;
-  uint8_t* const codes_t = o.codes_t ? o.codes_t + (b * o.cols) * op.pitch_t : nullptr;
-  uint8_t* const scales_r = o.scales_r + b * op.sf_r;
-  uint8_t* const scales_t = o.scales_t + b * op.sf_t;
   // codes of the thread's 8 rows x 8 columns go into shared memory as 8 columns x 8 rows; piece (8 rows) XOR column / 8, so that
   // the 16 lanes of a row, 8 columns apart, meet all banks
   const int piece = (warp * 2 + half) ^ l16;
   uint32_t square_code = 0u;
-
   if (o.square) {
     uint32_t m = 0u;
 #pragma unroll
@@ -186,24 +243,28 @@ __global__ void __launch_bounds__(256) quantize_fp8_kernel(const __grid_constant
     for (int q = 0; q < 8; ++q) m = max(m, col_bits[0][q]);
     square_code = fp8_scale_code(m);
   }
-  if (codes_r) {
+  if (o.codes_r) {
+    uint32_t code = square_code;                         // of row l16 / 2 (bits 3, 2, 1 of the lane)
+    if (!o.square) {
+      uint32_t m[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m[i] = v.row_max(i);
+      code = fp8_scale_code(own_row_max(m, l16));
+    }
+    if (!(lane & 1)) store_scale(o.scales_r + b * op.sf_r, row + (l16 >> 1), o.rows, ct, op.col_tiles, ops.swizzled, code);
+    const float own = fp8_scale_inverse(code);
+    uint8_t* dst = o.codes_r + (b * o.rows + row) * op.pitch_r + col;
+    const int rows = (int)min((int64_t)8, o.rows - row);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      uint32_t code = square_code;
-      if (!o.square) {
-        uint32_t m = v.row_max(i);
-#pragma unroll
-        for (int d = 8; d; d >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-        code = fp8_scale_code(m);
-      }
-      const float inv = fp8_scale_inverse(code);
-      const uint32_t lo = e4m3x4(v.get(i, 0) * inv, v.get(i, 1) * inv, v.get(i, 2) * inv, v.get(i, 3) * inv);
-      const uint32_t hi = e4m3x4(v.get(i, 4) * inv, v.get(i, 5) * inv, v.get(i, 6) * inv, v.get(i, 7) * inv);
-      if (row + i < o.rows && col < op.pitch_r) *reinterpret_cast<uint2*>(codes_r + (row + i) * op.pitch_r + col) = make_uint2(lo, hi);
-      if (l16 == i) store_scale(scales_r, row + i, o.rows, ct, op.nb_r, ops.swizzled, code);
+      const float inv = __shfl_sync(0xFFFFFFFFu, own, 2 * i, 16);
+      const uint32_t lo = scaled_codes(v.get(i, 0), v.get(i, 1), v.get(i, 2), v.get(i, 3), inv);
+      const uint32_t hi = scaled_codes(v.get(i, 4), v.get(i, 5), v.get(i, 6), v.get(i, 7), inv);
+      if (i < rows) store_codes(dst, left, lo, hi);
+      dst += op.pitch_r;
     }
   }
-  if (codes_t) {
+  if (o.codes_t) {
     if (!o.square) {
       uint32_t m[8];
       v.col_max(m);
@@ -226,23 +287,30 @@ __global__ void __launch_bounds__(256) quantize_fp8_kernel(const __grid_constant
         code = fp8_scale_code(m);
       }
       col_inverse[c] = fp8_scale_inverse(code);
-      store_scale(scales_t, c0 + c, o.cols, rt, op.nb_t, ops.swizzled, code);
+      store_scale(o.scales_t + b * op.sf_t, c0 + c, o.cols, rt, op.row_tiles, ops.swizzled, code);
     }
     __syncthreads();
+    float inv[8];
+#pragma unroll
+    for (int j = 0; j < 8; j += 4) *reinterpret_cast<float4*>(inv + j) = *reinterpret_cast<const float4*>(col_inverse + l16 * 8 + j);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float inv = col_inverse[l16 * 8 + j];
-      const uint32_t lo = e4m3x4(v.get(0, j) * inv, v.get(1, j) * inv, v.get(2, j) * inv, v.get(3, j) * inv);
-      const uint32_t hi = e4m3x4(v.get(4, j) * inv, v.get(5, j) * inv, v.get(6, j) * inv, v.get(7, j) * inv);
+      const uint32_t lo = scaled_codes(v.get(0, j), v.get(1, j), v.get(2, j), v.get(3, j), inv[j]);
+      const uint32_t hi = scaled_codes(v.get(4, j), v.get(5, j), v.get(6, j), v.get(7, j), inv[j]);
       *reinterpret_cast<uint2*>(turned + (l16 * 8 + j) * 128 + piece * 8) = make_uint2(lo, hi);
     }
     __syncthreads();
+    // a half warp takes columns warp * 2 + half + 16 i
+    const int c = warp * 2 + half;
+    const int rows = (int)min((int64_t)8, o.rows - r0 - l16 * 8);
+    uint8_t* dst = o.codes_t + (b * o.cols + c0 + c) * op.pitch_t + r0 + l16 * 8;
+    const int cols = (int)min((int64_t)128, o.cols - c0);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int c = i * 16 + warp * 2 + half;
-      if (c0 + c < o.cols && r0 + l16 * 8 < op.pitch_t)
-        *reinterpret_cast<uint2*>(codes_t + (c0 + c) * op.pitch_t + r0 + l16 * 8) =
-            *reinterpret_cast<const uint2*>(turned + c * 128 + ((l16 ^ (c >> 3)) * 8));
+      const int at = i * 16 + c;
+      const uint2 q = *reinterpret_cast<const uint2*>(turned + at * 128 + ((l16 ^ (at >> 3)) * 8));
+      if (at < cols) store_codes(dst, rows, q.x, q.y);
+      dst += 16 * op.pitch_t;
     }
   }
 }
@@ -264,14 +332,13 @@ int quantize_fp8(const Fp8Operand* list, int n, int dtype, int sf_layout, cudaSt
     Fp8Op& op = ops.op[i];
     const Fp8Operand& o = op.o = list[i];
     op.pitch_r = fp8_pitch(o.cols); op.pitch_t = fp8_pitch(o.rows);
-    op.nb_r = fp8_blocks(o.cols); op.nb_t = fp8_blocks(o.rows);
     op.sf_r = (int64_t)nvfp4_sf_bytes_fp8(o.rows, o.cols, sf_layout); op.sf_t = (int64_t)nvfp4_sf_bytes_fp8(o.cols, o.rows, sf_layout);
-    op.col_tiles = op.nb_r; op.row_tiles = op.nb_t;
-    op.first = tiles;
+    op.col_tiles = (int)fp8_blocks(o.cols); op.row_tiles = (int)fp8_blocks(o.rows);
+    op.first = (int)tiles;
     tiles += o.batch * op.col_tiles * op.row_tiles;
+    if (tiles > 0x7FFFFFFFll) return NVFP4_ERR_SHAPE;
     weighted = weighted || o.from.weights;
   }
-  if (tiles > 0x7FFFFFFFll) return NVFP4_ERR_SHAPE;
   if (dtype == NVFP4_BF16) return weighted ? launch<__nv_bfloat16, true>(ops, tiles, s) : launch<__nv_bfloat16, false>(ops, tiles, s);
   return weighted ? launch<float, true>(ops, tiles, s) : launch<float, false>(ops, tiles, s);
 }
