@@ -395,8 +395,8 @@ NVFP4_API int64_t nvfp4_expert_rows(int64_t tokens, int64_t topk, int64_t expert
 NVFP4_API int nvfp4_expert_sort(const void* expert_of, int wide, int64_t tokens, int64_t topk, int64_t experts, int32_t* counts,
                       int32_t* offsets, int32_t* row_of, int32_t* slot_of, void* cuda_stream);
 NVFP4_API int nvfp4_expert_gather(const void* x, int dtype, int64_t tokens, int64_t topk, int64_t experts, int64_t cols, int64_t ld,
-                        const int32_t* offsets, const int32_t* slot_of, const void* weights, int weights_dtype, void* rows,
-                        void* cuda_stream);
+                        const int32_t* offsets, const int32_t* slot_of, const int32_t* row_of, const void* weights,
+                        int weights_dtype, void* rows, void* cuda_stream);
 NVFP4_API int nvfp4_expert_combine(const void* rows, int dtype, int64_t tokens, int64_t topk, int64_t experts, int64_t cols,
                          const int32_t* row_of, const void* weights, int weights_dtype, void* y, void* cuda_stream);
 NVFP4_API int nvfp4_expert_combine_bwd(const void* dy, int dtype, int64_t tokens, int64_t topk, int64_t experts, int64_t cols, int64_t ld,

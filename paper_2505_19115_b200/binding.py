@@ -125,7 +125,7 @@ def lib():
     L.nvfp4_expert_sort.restype = ci
     L.nvfp4_expert_sort.argtypes = [vp, ci, i64, i64, i64, vp, vp, vp, vp, vp]
     L.nvfp4_expert_gather.restype = ci
-    L.nvfp4_expert_gather.argtypes = [vp, ci, i64, i64, i64, i64, i64, vp, vp, vp, ci, vp, vp]
+    L.nvfp4_expert_gather.argtypes = [vp, ci, i64, i64, i64, i64, i64, vp, vp, vp, vp, ci, vp, vp]
     L.nvfp4_expert_combine.restype = ci
     L.nvfp4_expert_combine.argtypes = [vp, ci, i64, i64, i64, i64, vp, vp, ci, vp, vp]
     L.nvfp4_expert_combine_bwd.restype = ci
@@ -667,7 +667,7 @@ def nvfp4_expert_gather(x, plan, weights=None, out=None, stream=None):
     assert out.is_contiguous() and out.shape == (plan.rows, cols) and out.dtype == x.dtype
     w, w_dtype = _weights(weights, plan)
     st = _native().nvfp4_expert_gather(x, x, plan.tokens, plan.topk, plan.experts, cols, x.stride(0) if plan.tokens > 1 else cols,
-                                       plan.offsets, plan.slot_of, w, w_dtype, out, stream)
+                                       plan.offsets, plan.slot_of, plan.row_of, w, w_dtype, out, stream)
     _check(st, "nvfp4_expert_gather")
     return out
 

@@ -22,7 +22,7 @@ namespace cg = cooperative_groups;
 // ------------------------------------------------------------------------------------------------
 // Sort.  Bound by latency: 4 or 8 bytes read and 8 written per slot.  One launch: a cluster of up to eight blocks (the slots cut
 // into as many ranges, each cut into one per warp).  A warp counts its range per expert (lanes with the same expert find one
-// another with a match), the counts become running sums over the warps, the blocks read one another's totals from shared
+// another by votes), the counts become running sums over the warps, the blocks read one another's totals from shared
 // memory, every block computes all offsets, and each warp goes over its range again and hands out rows.
 // ------------------------------------------------------------------------------------------------
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kMaxCluster = 8;
@@ -36,16 +36,30 @@ struct SortParams {
   int32_t *counts, *offsets, *row_of, *slot_of;
 };
 
+// The lanes that carry the same expert (meaningless for a dropped slot): a vote for each of its bits.  262144 slots, 64 experts, with one
+// match instruction instead, of which a multiprocessor does one in about 60 cycles: 70 us; so: 50.
+__device__ __forceinline__ unsigned same_expert(int e, int bits) {
+  unsigned same = __ballot_sync(0xFFFFFFFFu, e >= 0);
+  for (int b = 0; b < bits; ++b) {
+    const bool bit = (e >> b) & 1;
+    const unsigned set = __ballot_sync(0xFFFFFFFFu, bit);
+    same &= bit ? set : ~set;
+  }
+  return same;
+}
+
 __global__ void __launch_bounds__(kSortThreads, 1) expert_sort_kernel(const SortParams p) {
-  extern __shared__ int hist[];                      // [kSortWarps][experts], then totals[experts], base[experts], offset[experts + 1]
+  extern __shared__ int hist[];                      // [kSortWarps][stride], then totals, base, end [experts] and offset [experts + 1]
   __shared__ int warp_sum[kSortWarps];
   cg::cluster_group cluster = cg::this_cluster();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int E = p.experts;
-  int* const totals = hist + kSortWarps * E;
+  const int E = p.experts, bits = 32 - __clz(E - 1);   // an expert's number
+  const int stride = E | 1;                          // odd: 32 warps' counts of an expert lie in 32 banks
+  int* const totals = hist + kSortWarps * stride;
   int* const base = totals + E;
-  int* const offset = base + E;
-  int* const mine = hist + warp * E;
+  int* const end = base + E;
+  int* const offset = end + E;
+  int* const mine = hist + warp * stride;
   for (int e = lane; e < E; e += 32) mine[e] = 0;
   __syncwarp();
   grid_dependency_wait();
@@ -58,32 +72,43 @@ __global__ void __launch_bounds__(kSortThreads, 1) expert_sort_kernel(const Sort
     const long long e = p.wide ? reinterpret_cast<const volatile long long*>(p.expert_of)[s] : reinterpret_cast<const volatile int32_t*>(p.expert_of)[s];
     return e >= 0 && e < E ? (int)e : -1;
   };
-  int next = expert_at(first + lane);
-  for (int s = first; s < last; s += 32) {
-    const int e = next;
-    next = expert_at(s + 32 + lane);
-    const unsigned same = __match_any_sync(0xFFFFFFFFu, e);
-    if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
-    __syncwarp();
+  // four loads in flight; a range of up to 128 slots stays in registers for the second pass
+  int at[4];
+  auto fetch = [&](int s0) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) at[q] = expert_at(s0 + 32 * q + lane);
+  };
+  for (int s0 = first; s0 < last; s0 += 128) {
+    fetch(s0);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (s0 + 32 * q >= last) break;
+      const unsigned same = same_expert(at[q], bits);
+      if (at[q] >= 0 && lane == __ffs(same) - 1) mine[at[q]] += __popc(same);
+      __syncwarp();
+    }
   }
   __syncthreads();
-  // running sums over the warps; this block's total of every expert
-  for (int e = threadIdx.x; e < E; e += kSortThreads) {
-    int sum = 0;
-    for (int w = 0; w < kSortWarps; ++w) {
-      const int c = hist[w * E + e];
-      hist[w * E + e] = sum;
-      sum += c;
+  // running sums over the warps (a lane each); this block's total of every expert
+  for (int e = warp; e < E; e += kSortWarps) {
+    const int c = hist[lane * stride + e];
+    int sum = c;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int up = __shfl_up_sync(0xFFFFFFFFu, sum, d);
+      if (lane >= d) sum += up;
     }
-    totals[e] = sum;
+    hist[lane * stride + e] = sum - c;
+    if (lane == 31) totals[e] = sum;
   }
   cluster.sync();
   // offsets of all segments (an expert per thread), and where this block's rows of an expert begin
   const int e = threadIdx.x;
   int before = 0, count = 0;
   if (e < E) {
-    for (unsigned c = 0; c < cluster.num_blocks(); ++c) {
-      const int other = *cluster.map_shared_rank(totals + e, c);
+#pragma unroll
+    for (unsigned c = 0; c < kMaxCluster; ++c) {
+      const int other = c < cluster.num_blocks() ? *cluster.map_shared_rank(totals + e, c) : 0;
       if (c < cluster.block_rank()) before += other;
       count += other;
     }
@@ -117,24 +142,29 @@ __global__ void __launch_bounds__(kSortThreads, 1) expert_sort_kernel(const Sort
       p.offsets[e] = begin;
       if (e == E - 1) p.offsets[E] = begin + padded;
     }
-    // padding of the segment: rows behind its last slot
-    if (e % cluster.num_blocks() == cluster.block_rank())
-      for (int r = begin + count; r < begin + padded; ++r) p.slot_of[r] = -1;
+    end[e] = begin + count;
   }
   __syncthreads();
-  next = expert_at(first + lane);
-  for (int s = first; s < last; s += 32) {
-    const int x = next;
-    next = expert_at(s + 32 + lane);
-    const unsigned same = __match_any_sync(0xFFFFFFFFu, x);
-    int row = -1;
-    if (x >= 0) row = base[x] + mine[x] + __popc(same & ((1u << lane) - 1u));
-    __syncwarp();
-    if (x >= 0 && lane == __ffs(same) - 1) mine[x] += __popc(same);
-    __syncwarp();
-    if (s + lane < last) {
-      p.row_of[s + lane] = row;
-      if (row >= 0) p.slot_of[row] = s + lane;
+  // padding of the segments: rows behind their last slots
+  for (int s = cluster.block_rank() * kSortWarps + warp; s < E; s += kSortWarps * cluster.num_blocks())
+    for (int r = end[s] + lane; r < offset[s + 1]; r += 32) p.slot_of[r] = -1;
+  for (int s0 = first; s0 < last; s0 += 128) {
+    if (last - first > 128) fetch(s0);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int s = s0 + 32 * q;
+      if (s >= last) break;
+      const int x = at[q];
+      const unsigned same = same_expert(x, bits);
+      int row = -1;
+      if (x >= 0) row = base[x] + mine[x] + __popc(same & ((1u << lane) - 1u));
+      __syncwarp();
+      if (x >= 0 && lane == __ffs(same) - 1) mine[x] += __popc(same);
+      __syncwarp();
+      if (s + lane < last) {
+        p.row_of[s + lane] = row;
+        if (row >= 0) p.slot_of[row] = s + lane;
+      }
     }
   }
   for (int r = offset[E] + cluster.block_rank() * kSortThreads + threadIdx.x; r < p.rows; r += kSortThreads * cluster.num_blocks()) p.slot_of[r] = -1;
@@ -142,39 +172,41 @@ __global__ void __launch_bounds__(kSortThreads, 1) expert_sort_kernel(const Sort
 }
 
 // ------------------------------------------------------------------------------------------------
-// Moving rows.  All three are bound by memory; 8 values (16 or 32 bytes) of a row per lane and step.
+// Moving rows.  All three are bound by memory, in units of 16 bytes of a row.  What they read first are indices, so a warp fetches
+// all that it needs at once (a lane each) and then has 4 to 8 units per lane in flight.
 // ------------------------------------------------------------------------------------------------
 template <typename T>
-struct Vec8 {
-  float v[8];
-  __device__ __forceinline__ void load(const T* src) {
-    const uint4 a = load_vec16(src);
-    if constexpr (std::is_same_v<T, float>) {
-      const uint4 b = load_vec16(src + 4);
-      const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+constexpr int kUnit = 16 / (int)sizeof(T);           // values per unit
+template <typename T>
+__device__ __forceinline__ void unpack(const uint4& u, float (&v)[kUnit<T>]) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
-    } else {
-      const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(w[i]);
+    else { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+  }
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack(const float (&v)[kUnit<T>]) {
+  uint32_t w[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(v[i]);
+    else {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
     }
   }
-  __device__ __forceinline__ void store(T* dst) const {
-    if constexpr (std::is_same_v<T, float>) {
-      reinterpret_cast<float4*>(dst)[0] = make_float4(v[0], v[1], v[2], v[3]);
-      reinterpret_cast<float4*>(dst)[1] = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-      uint32_t w[4];
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <typename T>
+__device__ __forceinline__ uint4 scaled(const uint4& u, float w) {
+  float v[kUnit<T>];
+  unpack<T>(u, v);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        w[i] = *reinterpret_cast<const uint32_t*>(&h);
-      }
-      *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-  }
-};
+  for (int i = 0; i < kUnit<T>; ++i) v[i] = __fmul_rn(v[i], w);
+  return pack<T>(v);
+}
 
 // A weight that the kernel before this one may have written.
 __device__ __forceinline__ float weight_at(const void* w, int dtype, int64_t i) {
@@ -193,139 +225,231 @@ struct MoveParams {
   const int32_t *slot_of, *row_of, *used;
   int64_t tokens, n_rows, cols, ld;
   int topk, weights_dtype;
-  int64_t pieces;               // per row
+  int units;                    // of a row
+  int item_blocks;              // blocks that move rows, in front of those that clear padding
+  int piece_bits;               // gradient of the combination
 };
 
 constexpr int kMoveWarps = 8;
-constexpr int kGatherCols = 1024, kCombineCols = 256;
 
-// One warp moves up to 1024 columns of a row.
-template <typename T>
-__global__ void __launch_bounds__(32 * kMoveWarps) expert_gather_kernel(const MoveParams p) {
+// Clears the padding rows among the eight that this warp looks at; gridDim.y warps share them.  block: among those that do this.
+__device__ __forceinline__ void clear_padding(const MoveParams& p, void* rows, int64_t row_units, int64_t block) {
   const int lane = threadIdx.x & 31;
-  const int64_t item = (int64_t)blockIdx.x * kMoveWarps + (threadIdx.x >> 5);
-  const int64_t r = item / p.pieces, c0 = (item - r * p.pieces) * kGatherCols + lane * 8;
-  grid_dependency_wait();
-  grid_dependency_trigger();
-  if (r >= p.n_rows || r >= int_at(p.used, 0)) return;
-  int slot = int_at(p.slot_of, r);
-  if (slot >= p.tokens * p.topk) slot = -1;          // no such slot
-  const float w = slot >= 0 ? weight_at(p.weights, p.weights_dtype, slot) : 0.0f;
-  const T* const src = static_cast<const T*>(p.x) + (int64_t)(slot < 0 ? 0 : slot / p.topk) * p.ld + c0;
-  T* const dst = static_cast<T*>(p.out) + r * p.cols + c0;
-  Vec8<T> v[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v[i].v[q] = 0.0f;
-    if (slot >= 0 && c0 + 256 * i < p.cols) v[i].load(src + 256 * i);
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (c0 + 256 * i >= p.cols) break;
-    if (p.weights) {
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v[i].v[q] = slot >= 0 ? __fmul_rn(v[i].v[q], w) : 0.0f;
-    }
-    v[i].store(dst + 256 * i);
+  const int64_t r0 = (block * kMoveWarps + (threadIdx.x >> 5)) * 8;
+  const int64_t used = min((int64_t)int_at(p.used, 0), p.n_rows);
+  unsigned pads = __ballot_sync(0xFFFFFFFFu, lane < 8 && r0 + lane < used && int_at(p.slot_of, min(r0 + lane, p.n_rows - 1)) < 0);
+  for (; pads; pads &= pads - 1) {
+    uint4* const row = static_cast<uint4*>(rows) + (r0 + __ffs(pads) - 1) * row_units;
+    for (int u = blockIdx.y * 32 + lane; u < p.units; u += gridDim.y * 32) row[u] = make_uint4(0, 0, 0, 0);
   }
 }
 
-// One warp computes 256 columns of a token.
-template <typename T>
+// A warp takes a token, so that its row is read once, and stores it to the rows of its choices, 32 * U units at a time; gridDim.y
+// warps share it.  The blocks behind those clear padding rows.
+template <typename T, int U>
+__global__ void __launch_bounds__(32 * kMoveWarps, 4) expert_gather_kernel(const MoveParams p) {
+  const int lane = threadIdx.x & 31;
+  grid_dependency_wait();
+  grid_dependency_trigger();
+  if (blockIdx.x >= (unsigned)p.item_blocks) return clear_padding(p, p.out, p.units, blockIdx.x - p.item_blocks);
+  const int64_t t = (int64_t)blockIdx.x * kMoveWarps + (threadIdx.x >> 5);
+  if (t >= p.tokens) return;
+  const uint4* const src = reinterpret_cast<const uint4*>(static_cast<const T*>(p.x) + t * p.ld);
+  for (int u0 = blockIdx.y * 32 * U + lane; u0 - lane < p.units; u0 += gridDim.y * 32 * U) {
+    uint4 v[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) v[i] = u0 + 32 * i < p.units ? load_vec16(src + u0 + 32 * i) : make_uint4(0, 0, 0, 0);
+    for (int j0 = 0; j0 < p.topk; j0 += 32) {        // a lane fetches the row and the weight of a choice
+      int row = -1;
+      float weight = 1.0f;
+      if (j0 + lane < p.topk) {
+        const int64_t s = t * p.topk + j0 + lane;
+        row = int_at(p.row_of, s);
+        weight = weight_at(p.weights, p.weights_dtype, s);
+        if (row >= p.n_rows) row = -1;               // no such row
+      }
+      const int n = min(32, p.topk - j0);
+      for (int j = 0; j < n; ++j) {
+        const int to = __shfl_sync(0xFFFFFFFFu, row, j);
+        const float w = __shfl_sync(0xFFFFFFFFu, weight, j);
+        if (to < 0) continue;
+        uint4* const dst = static_cast<uint4*>(p.out) + (int64_t)to * p.units;
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+          if (u0 + 32 * i < p.units) dst[u0 + 32 * i] = p.weights ? scaled<T>(v[i], w) : v[i];
+      }
+    }
+  }
+}
+
+// A warp computes a token, 32 * U units at a time of J rows at a time; gridDim.y warps share it.
+template <typename T, int U, int J>
 __global__ void __launch_bounds__(32 * kMoveWarps) expert_combine_kernel(const MoveParams p) {
   const int lane = threadIdx.x & 31;
-  const int64_t item = (int64_t)blockIdx.x * kMoveWarps + (threadIdx.x >> 5);
-  const int64_t t = item / p.pieces, c = (item - t * p.pieces) * kCombineCols + lane * 8;
+  const int64_t t = (int64_t)blockIdx.x * kMoveWarps + (threadIdx.x >> 5);
+  if (t >= p.tokens) return;
   grid_dependency_wait();
   grid_dependency_trigger();
-  if (t >= p.tokens || c >= p.cols) return;
-  float sum[8] = {};
-  for (int j0 = 0; j0 < p.topk; j0 += 4) {           // four rows in flight
-    Vec8<T> v[4];
-    float w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t s = t * p.topk + j0 + j;
-      int r = j0 + j < p.topk ? int_at(p.row_of, s) : -1;
-      if (r >= p.n_rows) r = -1;                     // no such row
-      w[j] = r >= 0 ? weight_at(p.weights, p.weights_dtype, s) : 0.0f;
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v[j].v[q] = 0.0f;
-      if (r >= 0) v[j].load(static_cast<const T*>(p.rows) + (int64_t)r * p.cols + c);
+  int row = -1;                                      // of the lane's choice, of 32 at a time
+  float weight = 0.0f;
+  auto fetch = [&](int j0) {
+    row = -1;
+    if (j0 + lane < p.topk) {
+      const int64_t s = t * p.topk + j0 + lane;
+      row = int_at(p.row_of, s);
+      weight = weight_at(p.weights, p.weights_dtype, s);
+      if (row >= p.n_rows) row = -1;                 // no such row
     }
+  };
+  fetch(0);
+  uint4* const dst = reinterpret_cast<uint4*>(static_cast<T*>(p.out) + t * p.cols);
+  for (int u = blockIdx.y * 32 * U; u < p.units; u += gridDim.y * 32 * U) {
+    const int u0 = u + lane;
+    float sum[U][kUnit<T>] = {};
+    for (int j0 = 0; j0 < p.topk; j0 += 32) {
+      if (p.topk > 32) fetch(j0);
+      const int n = min(32, p.topk - j0);
+      for (int j = 0; j < n; j += J) {
+        uint4 v[J][U];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+        for (int q = 0; q < J; ++q) {
+          const int from = j + q < n ? __shfl_sync(0xFFFFFFFFu, row, j + q) : -1;
+          const uint4* const src = reinterpret_cast<const uint4*>(static_cast<const T*>(p.rows) + (int64_t)max(from, 0) * p.cols);
 #pragma unroll
-      for (int q = 0; q < 8; ++q) sum[q] = __fmaf_rn(w[j], v[j].v[q], sum[q]);
-  }
-  Vec8<T> out;
+          for (int i = 0; i < U; ++i) v[q][i] = from >= 0 && u0 + 32 * i < p.units ? load_vec16(src + u0 + 32 * i) : make_uint4(0, 0, 0, 0);
+        }
 #pragma unroll
-  for (int q = 0; q < 8; ++q) out.v[q] = sum[q];
-  out.store(static_cast<T*>(p.out) + t * p.cols + c);
-}
-
-// One warp takes a slot (in the order of tokens: a token's row of dy comes from memory once); the warps behind those look at 32
-// rows each and clear the padding rows among them.
-template <typename T>
-__global__ void __launch_bounds__(32 * kMoveWarps) expert_combine_bwd_kernel(const MoveParams p) {
-  const int lane = threadIdx.x & 31;
-  const int64_t slots = p.tokens * p.topk, item = (int64_t)blockIdx.x * kMoveWarps + (threadIdx.x >> 5);
-  grid_dependency_wait();
-  grid_dependency_trigger();
-  if (item < slots) {
-    int r = int_at(p.row_of, item);
-    if (r >= p.n_rows) r = -1;                       // no such row
-    float dot = 0.0f;
-    if (r >= 0) {
-      const float w = weight_at(p.weights, p.weights_dtype, item);
-      const T* const dy = static_cast<const T*>(p.x) + item / p.topk * p.ld;
-      const T* const row = static_cast<const T*>(p.rows) + (int64_t)r * p.cols;
-      T* const drow = p.drows ? static_cast<T*>(p.drows) + (int64_t)r * p.cols : nullptr;
-      for (int64_t c = lane * 8; c < p.cols; c += 1024) {
-        Vec8<T> a[4], b[4];
+        for (int q = 0; q < J; ++q) {
+          if (j + q >= n || __shfl_sync(0xFFFFFFFFu, row, j + q) < 0) continue;
+          const float w = __shfl_sync(0xFFFFFFFFu, weight, j + q);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (c + 256 * i < p.cols) { a[i].load(dy + c + 256 * i); b[i].load(row + c + 256 * i); }
+          for (int i = 0; i < U; ++i) {
+            float x[kUnit<T>];
+            unpack<T>(v[q][i], x);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (c + 256 * i >= p.cols) break;
-#pragma unroll
-          for (int q = 0; q < 8; ++q) dot = __fmaf_rn(a[i].v[q], b[i].v[q], dot);
-          if (drow) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) a[i].v[q] = __fmul_rn(a[i].v[q], w);
-            a[i].store(drow + c + 256 * i);
+            for (int e = 0; e < kUnit<T>; ++e) sum[i][e] = __fmaf_rn(w, x[e], sum[i][e]);
           }
         }
       }
-#pragma unroll
-      for (int d = 16; d; d >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, d);
     }
-    if (lane == 0) {
-      if (p.weights_dtype == NVFP4_BF16) static_cast<__nv_bfloat16*>(p.dweights)[item] = __float2bfloat16_rn(dot);
-      else static_cast<float*>(p.dweights)[item] = dot;
-    }
-    return;
-  }
-  if (!p.drows) return;
-  const int64_t r0 = (item - slots) * 32;
-  const int64_t used = min((int64_t)int_at(p.used, 0), p.n_rows);
-  unsigned pads = __ballot_sync(0xFFFFFFFFu, r0 + lane < used && int_at(p.slot_of, min(r0 + lane, p.n_rows - 1)) < 0);
-  Vec8<T> zero;
 #pragma unroll
-  for (int q = 0; q < 8; ++q) zero.v[q] = 0.0f;
-  for (; pads; pads &= pads - 1) {
-    T* const drow = static_cast<T*>(p.drows) + (r0 + __ffs(pads) - 1) * p.cols;
-    for (int64_t c = lane * 8; c < p.cols; c += 256) zero.store(drow + c);
+    for (int i = 0; i < U; ++i)
+      if (u0 + 32 * i < p.units) dst[u0 + 32 * i] = pack<T>(sum[i]);
   }
 }
 
+// 2^piece_bits warps of a block take J choices of a token (in the order of tokens: a row of dy comes from memory once), 32 * U units of
+// all rows each at a time, and join their parts of the products in shared memory; the blocks behind those look at eight rows a warp
+// and clear the padding rows among them.
+template <typename T, int J, int U>
+__global__ void __launch_bounds__(32 * kMoveWarps, 3) expert_combine_bwd_kernel(const MoveParams p) {
+  __shared__ float parts[J][kMoveWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const unsigned groups = (p.topk + J - 1) / J;
+  grid_dependency_wait();
+  grid_dependency_trigger();
+  if (blockIdx.x < (unsigned)p.item_blocks) {
+    const int piece = warp & ((1 << p.piece_bits) - 1);
+    // items are fewer than slots: 32 bits
+    const unsigned item = blockIdx.x * (kMoveWarps >> p.piece_bits) + (warp >> p.piece_bits), t = item / groups, j0 = (item - t * groups) * J;
+    const int n = t < p.tokens ? min(J, (int)(p.topk - j0)) : 0;
+    const int64_t s0 = (int64_t)t * p.topk + j0;
+    const uint4* const dy = reinterpret_cast<const uint4*>(static_cast<const T*>(p.x) + (int64_t)(n ? t : 0) * p.ld);
+    int r[J];
+    float w[J], dot[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      r[j] = j < n ? int_at(p.row_of, s0 + j) : -1;
+      w[j] = j < n ? weight_at(p.weights, p.weights_dtype, s0 + j) : 0.0f;
+      if (r[j] >= p.n_rows) r[j] = -1;               // no such row
+      dot[j] = 0.0f;
+    }
+    for (int u0 = piece * 32 * U + lane; u0 < p.units; u0 += (32 * U) << p.piece_bits) {
+      uint4 a[U], b[J][U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) a[i] = u0 + 32 * i < p.units ? load_vec16(dy + u0 + 32 * i) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const uint4* const row = reinterpret_cast<const uint4*>(static_cast<const T*>(p.rows) + (int64_t)max(r[j], 0) * p.cols);
+#pragma unroll
+        for (int i = 0; i < U; ++i) b[j][i] = r[j] >= 0 && u0 + 32 * i < p.units ? load_vec16(row + u0 + 32 * i) : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        if (r[j] < 0) continue;
+        uint4* const drow = p.drows ? reinterpret_cast<uint4*>(static_cast<T*>(p.drows) + (int64_t)r[j] * p.cols) : nullptr;
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          float x[kUnit<T>], y[kUnit<T>];
+          unpack<T>(a[i], x);
+          unpack<T>(b[j][i], y);
+#pragma unroll
+          for (int e = 0; e < kUnit<T>; ++e) dot[j] = __fmaf_rn(x[e], y[e], dot[j]);
+          if (drow && u0 + 32 * i < p.units) drow[u0 + 32 * i] = scaled<T>(a[i], w[j]);
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int d = 16; d; d >>= 1) dot[j] += __shfl_xor_sync(0xFFFFFFFFu, dot[j], d);
+    if (p.piece_bits) {
+      if (lane == 0)
+#pragma unroll
+        for (int j = 0; j < J; ++j) parts[j][warp] = dot[j];
+      __syncthreads();
+    }
+    if (piece != 0 || lane >= n) return;
+    float sum = dot[0];
+#pragma unroll
+    for (int j = 1; j < J; ++j)
+      if (lane == j) sum = dot[j];
+    for (int i = 1; i < 1 << p.piece_bits; ++i) sum += parts[lane][warp + i];
+    if (p.weights_dtype == NVFP4_BF16) static_cast<__nv_bfloat16*>(p.dweights)[s0 + lane] = __float2bfloat16_rn(sum);
+    else static_cast<float*>(p.dweights)[s0 + lane] = sum;
+    return;
+  }
+  clear_padding(p, p.drows, p.units, blockIdx.x - p.item_blocks);
+}
+
 template <typename Kernel>
-int launch_warps(Kernel kernel, int64_t warps, const MoveParams& p, cudaStream_t s) {
-  const int64_t blocks = ceil_div(warps, kMoveWarps);
-  if (blocks > 0x7FFFFFFFll) return NVFP4_ERR_SHAPE;
-  return launch_overlapped(kernel, dim3((unsigned)blocks), 32 * kMoveWarps, 0, s, p) == cudaSuccess ? NVFP4_OK : NVFP4_ERR_CUDA;
+int launch_blocks(Kernel kernel, int64_t blocks, int64_t pieces, const MoveParams& p, cudaStream_t s) {
+  if (blocks > 0x7FFFFFFFll || pieces > 65535) return NVFP4_ERR_SHAPE;
+  return launch_overlapped(kernel, dim3((unsigned)blocks, (unsigned)pieces), 32 * kMoveWarps, 0, s, p) == cudaSuccess ? NVFP4_OK : NVFP4_ERR_CUDA;
+}
+// Warps that share a row of `units`, 32 * u at a time: one where there are rows enough to fill the multiprocessors, since its indices
+// and addresses then cost least (16384 tokens, two choices, 2816 columns, us, eight warps -> one: combine 50 -> 45, gradient 104 -> 76).
+int64_t row_pieces(int64_t rows, int64_t units, int64_t u) {
+  return std::clamp<int64_t>(ceil_div(16 * sm_count(), rows), 1, std::min<int64_t>(ceil_div(units, 32 * u), 65535));
+}
+template <typename T>
+int combine(MoveParams p, cudaStream_t s) {
+  p.units = (int)(p.cols / kUnit<T>);
+  const int64_t blocks = ceil_div(p.tokens, kMoveWarps);
+  if (p.tokens < 16 * sm_count()) return launch_blocks(expert_combine_kernel<T, 1, 8>, blocks, row_pieces(p.tokens, p.units, 1), p, s);
+  return launch_blocks(expert_combine_kernel<T, 4, 2>, blocks, 1, p, s);
+}
+template <typename T>
+int gather(MoveParams p, cudaStream_t s) {
+  p.units = (int)(p.cols / kUnit<T>);
+  p.item_blocks = (int)ceil_div(p.tokens, kMoveWarps);
+  const int64_t blocks = p.item_blocks + ceil_div(p.n_rows, 8 * kMoveWarps);
+  if (p.tokens < 16 * sm_count()) return launch_blocks(expert_gather_kernel<T, 1>, blocks, row_pieces(p.tokens, p.units, 1), p, s);
+  return launch_blocks(expert_gather_kernel<T, 4>, blocks, 1, p, s);
+}
+template <typename T, int J, int U>
+int launch_combine_bwd(MoveParams p, cudaStream_t s) {
+  const int64_t items = p.tokens * ceil_div(p.topk, J);
+  // several warps for a row where there are few rows
+  for (p.piece_bits = 0; p.piece_bits < 3 && (32 * U << p.piece_bits) < p.units && (items << p.piece_bits) < 8 * sm_count();) ++p.piece_bits;
+  p.item_blocks = (int)ceil_div(items, kMoveWarps >> p.piece_bits);
+  return launch_blocks(expert_combine_bwd_kernel<T, J, U>, p.item_blocks + (p.drows ? ceil_div(p.n_rows, 8 * kMoveWarps) : 0), 1, p, s);
+}
+template <typename T>
+int combine_bwd(MoveParams p, cudaStream_t s) {
+  p.units = (int)(p.cols / kUnit<T>);
+  // two choices share a token's row of dy, once there are enough of them
+  return p.topk > 1 && p.tokens * p.topk >= 32 * sm_count() ? launch_combine_bwd<T, 2, 4>(p, s) : launch_combine_bwd<T, 1, 4>(p, s);
 }
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -361,9 +485,9 @@ extern "C" int nvfp4_expert_sort(const void* expert_of, int wide, int64_t tokens
   p.n = (int)n; p.experts = (int)experts; p.rows = (int)rows;
   p.per_warp = (int)(ceil_div(n, 32 * kSortWarps * cluster) * 32);
   p.counts = counts; p.offsets = offsets; p.row_of = row_of; p.slot_of = slot_of;
-  const size_t smem = sizeof(int) * ((kSortWarps + 3) * experts + 1);
+  const size_t smem = sizeof(int) * (kSortWarps * (experts | 1) + 4 * experts + 1);
   static DeviceFlags smem_set;
-  if (set_max_dynamic_smem(smem_set, expert_sort_kernel, (int)(sizeof(int) * ((kSortWarps + 3) * kMaxExperts + 1))) != cudaSuccess) return NVFP4_ERR_CUDA;
+  if (set_max_dynamic_smem(smem_set, expert_sort_kernel, (int)(sizeof(int) * (kSortWarps * (kMaxExperts | 1) + 4 * kMaxExperts + 1))) != cudaSuccess) return NVFP4_ERR_CUDA;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
@@ -377,22 +501,21 @@ extern "C" int nvfp4_expert_sort(const void* expert_of, int wide, int64_t tokens
 }
 
 extern "C" int nvfp4_expert_gather(const void* x, int dtype, int64_t tokens, int64_t topk, int64_t experts, int64_t cols, int64_t ld,
-                                   const int32_t* offsets, const int32_t* slot_of, const void* weights, int weights_dtype, void* rows,
-                                   void* cuda_stream) {
-  if (!x || !offsets || !slot_of || !rows) return NVFP4_ERR_NULL;
+                                   const int32_t* offsets, const int32_t* slot_of, const int32_t* row_of, const void* weights,
+                                   int weights_dtype, void* rows, void* cuda_stream) {
+  if (!x || !offsets || !slot_of || !row_of || !rows) return NVFP4_ERR_NULL;
   if (!dtype_ok(dtype) || !dtype_ok(weights_dtype)) return NVFP4_ERR_ENUM;
   const int64_t n_rows = nvfp4_expert_rows(tokens, topk, experts);
-  if (n_rows == 0 || cols <= 0 || cols % 8 != 0 || ld < cols) return NVFP4_ERR_SHAPE;
-  if (!aligned16(x) || !aligned16(rows) || ld % 8 != 0 || !aligned4(offsets) || !aligned4(slot_of) || !aligned_for(weights, weights_dtype))
+  if (n_rows == 0 || cols <= 0 || cols % 8 != 0 || ld < cols || cols > (1ll << 31) - 512) return NVFP4_ERR_SHAPE;
+  if (!aligned16(x) || !aligned16(rows) || ld % 8 != 0 || !aligned4(offsets) || !aligned4(slot_of) || !aligned4(row_of) ||
+      !aligned_for(weights, weights_dtype))
     return NVFP4_ERR_ALIGN;
   if (int st = check_arch()) return st;
   MoveParams p = {};
-  p.x = x; p.weights = weights; p.out = rows; p.slot_of = slot_of; p.used = offsets + experts;
+  p.x = x; p.weights = weights; p.out = rows; p.slot_of = slot_of; p.row_of = row_of; p.used = offsets + experts;
   p.tokens = tokens; p.n_rows = n_rows; p.cols = cols; p.ld = ld; p.topk = (int)topk; p.weights_dtype = weights_dtype;
-  p.pieces = ceil_div(cols, kGatherCols);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  return dtype == NVFP4_BF16 ? launch_warps(expert_gather_kernel<__nv_bfloat16>, n_rows * p.pieces, p, s)
-                             : launch_warps(expert_gather_kernel<float>, n_rows * p.pieces, p, s);
+  return dtype == NVFP4_BF16 ? gather<__nv_bfloat16>(p, s) : gather<float>(p, s);
 }
 
 extern "C" int nvfp4_expert_combine(const void* rows, int dtype, int64_t tokens, int64_t topk, int64_t experts, int64_t cols,
@@ -400,16 +523,14 @@ extern "C" int nvfp4_expert_combine(const void* rows, int dtype, int64_t tokens,
   if (!rows || !row_of || !y) return NVFP4_ERR_NULL;
   if (!dtype_ok(dtype) || !dtype_ok(weights_dtype)) return NVFP4_ERR_ENUM;
   const int64_t n_rows = nvfp4_expert_rows(tokens, topk, experts);
-  if (n_rows == 0 || cols <= 0 || cols % 8 != 0) return NVFP4_ERR_SHAPE;
+  if (n_rows == 0 || cols <= 0 || cols % 8 != 0 || cols > (1ll << 31) - 512) return NVFP4_ERR_SHAPE;
   if (!aligned16(rows) || !aligned16(y) || !aligned4(row_of) || !aligned_for(weights, weights_dtype)) return NVFP4_ERR_ALIGN;
   if (int st = check_arch()) return st;
   MoveParams p = {};
   p.rows = rows; p.weights = weights; p.out = y; p.row_of = row_of;
   p.tokens = tokens; p.n_rows = n_rows; p.cols = cols; p.topk = (int)topk; p.weights_dtype = weights_dtype;
-  p.pieces = ceil_div(cols, kCombineCols);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  return dtype == NVFP4_BF16 ? launch_warps(expert_combine_kernel<__nv_bfloat16>, tokens * p.pieces, p, s)
-                             : launch_warps(expert_combine_kernel<float>, tokens * p.pieces, p, s);
+  return dtype == NVFP4_BF16 ? combine<__nv_bfloat16>(p, s) : combine<float>(p, s);
 }
 
 extern "C" int nvfp4_expert_combine_bwd(const void* dy, int dtype, int64_t tokens, int64_t topk, int64_t experts, int64_t cols, int64_t ld,
@@ -418,7 +539,7 @@ extern "C" int nvfp4_expert_combine_bwd(const void* dy, int dtype, int64_t token
   if (!dy || !offsets || !slot_of || !row_of || !rows || !weights || !dweights) return NVFP4_ERR_NULL;
   if (!dtype_ok(dtype) || !dtype_ok(weights_dtype)) return NVFP4_ERR_ENUM;
   const int64_t n_rows = nvfp4_expert_rows(tokens, topk, experts);
-  if (n_rows == 0 || cols <= 0 || cols % 8 != 0 || ld < cols) return NVFP4_ERR_SHAPE;
+  if (n_rows == 0 || cols <= 0 || cols % 8 != 0 || ld < cols || cols > (1ll << 31) - 512) return NVFP4_ERR_SHAPE;
   if (!aligned16(dy) || !aligned16(rows) || !aligned16(drows) || ld % 8 != 0 || !aligned4(offsets) || !aligned4(slot_of) || !aligned4(row_of) ||
       !aligned_for(weights, weights_dtype) || !aligned_for(dweights, weights_dtype))
     return NVFP4_ERR_ALIGN;
@@ -427,8 +548,6 @@ extern "C" int nvfp4_expert_combine_bwd(const void* dy, int dtype, int64_t token
   p.x = dy; p.rows = rows; p.weights = weights; p.drows = drows; p.dweights = dweights;
   p.slot_of = slot_of; p.row_of = row_of; p.used = offsets + experts;
   p.tokens = tokens; p.n_rows = n_rows; p.cols = cols; p.ld = ld; p.topk = (int)topk; p.weights_dtype = weights_dtype;
-  const int64_t warps = tokens * topk + (drows ? ceil_div(n_rows, 32) : 0);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  return dtype == NVFP4_BF16 ? launch_warps(expert_combine_bwd_kernel<__nv_bfloat16>, warps, p, s)
-                             : launch_warps(expert_combine_bwd_kernel<float>, warps, p, s);
+  return dtype == NVFP4_BF16 ? combine_bwd<__nv_bfloat16>(p, s) : combine_bwd<float>(p, s);
 }

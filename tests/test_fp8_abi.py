@@ -87,7 +87,7 @@ def test_routing_refusals():
     for status, changes in ((1, dict(e=None)), (1, dict(slot=None)), (4, dict(wide=2)), (2, dict(T=0)), (2, dict(E=1025)), (2, dict(k=0)), (3, dict(e=0x1002)), (3, dict(e=ODD, wide=1)),
                             (3, dict(row=0x1001))):
         _call("nvfp4_expert_sort", s, status, **changes)
-    g = dict(x=P, dtype=0, T=4, k=2, E=8, cols=64, ld=64, offsets=P, slot=P, w=P, wdtype=1, rows=P, stream=None)
+    g = dict(x=P, dtype=0, T=4, k=2, E=8, cols=64, ld=64, offsets=P, slot=P, row=P, w=P, wdtype=1, rows=P, stream=None)
     for status, changes in ((1, dict(x=None)), (1, dict(offsets=None)), (4, dict(dtype=3)), (4, dict(wdtype=3)), (2, dict(cols=60)), (2, dict(ld=56)), (2, dict(T=0)), (3, dict(x=ODD)),
                             (3, dict(ld=68)), (3, dict(w=0x1002)), (3, dict(rows=ODD))):
         _call("nvfp4_expert_gather", g, status, **changes)
