@@ -410,10 +410,11 @@ NVFP4_API int nvfp4_expert_combine_bwd(const void* dy, int dtype, int64_t tokens
  *   [tokens, cols] and gathered on the way; 0: x is [R, cols], sorted already.  Either way padding rows count as zero, whatever they
  *   hold, and rows are multiplied by weights (NULL: 1) before they are quantized.  Blocks along the rows never reach into another
  *   segment.  Codes of rows that are not used are not written.
- * nvfp4_gemm_fp8_experts: D[r] = A[r] . B[e]^T for the rows r of segment e; A [rows, K], B [experts, N, K] (codes and scales of the
- *   matrices one behind the other, as nvfp4_quantize_fp8 leaves a batch), D [rows, N].  rows = R.  For the input gradient B is the transposed
- *   output of the weights' quantization.
- * nvfp4_gemm_fp8_experts_dw: D[e] = A[:, segment e] . B[:, segment e]^T: A [N, rows] and B [K, rows], the transposed outputs of the
+ * nvfp4_gemm_fp8_experts: D[r] = A[r] . B[e]^T for the rows r of segment e; A [R, K], B [experts, N, K] (codes and scales of the
+ *   matrices one behind the other, as nvfp4_quantize_fp8 leaves a batch), D [R, N].  For the input gradient B is the transposed
+ *   output of the weights' quantization.  counts (NULL: unknown) lets calls with few rows for each expert read no padding; what
+ *   padding rows of D hold afterwards is not defined.
+ * nvfp4_gemm_fp8_experts_dw: D[e] = A[:, segment e] . B[:, segment e]^T: A [N, R] and B [K, R], the transposed outputs of the
  *   rows' quantization, D [experts, N, K] dense.  An expert without rows gets zeros.
  * nvfp4_experts_fp8_fwd / _bwd: the layer: Y [R, N] from X; dX [R, K] and dW [experts, N, K] from dY, W and X.  x_by_token / dy_by_token and
  *   dy_weights as by_token and weights above (the weighted sum's output gradient goes in as it is).  N and K multiples of 8, everything
@@ -423,10 +424,10 @@ NVFP4_API int nvfp4_quantize_fp8_experts(const void* x, int dtype, int by_token,
                                int64_t ld, const int32_t* offsets, const int32_t* slot_of, const void* weights, int weights_dtype,
                                uint8_t* codes_row, uint8_t* scales_row, uint8_t* codes_t, uint8_t* scales_t, void* cuda_stream);
 NVFP4_API int nvfp4_gemm_fp8_experts(const uint8_t* a_codes, const uint8_t* a_sf, const uint8_t* b_codes, const uint8_t* b_sf,
-                           int64_t experts, const int32_t* offsets, int64_t rows, int64_t N, int64_t K,
-                           void* d, int d_dtype, int64_t ldd, void* cuda_stream);
+                           int64_t tokens, int64_t topk, int64_t experts, const int32_t* counts, const int32_t* offsets,
+                           int64_t N, int64_t K, void* d, int d_dtype, int64_t ldd, void* cuda_stream);
 NVFP4_API int nvfp4_gemm_fp8_experts_dw(const uint8_t* a_codes, const uint8_t* a_sf, const uint8_t* b_codes, const uint8_t* b_sf,
-                              int64_t experts, const int32_t* offsets, int64_t rows, int64_t N, int64_t K,
+                              int64_t tokens, int64_t topk, int64_t experts, const int32_t* offsets, int64_t N, int64_t K,
                               void* d, int d_dtype, void* cuda_stream);
 NVFP4_API size_t nvfp4_experts_fp8_workspace_bytes(int64_t tokens, int64_t topk, int64_t experts, int64_t N, int64_t K, int which);
 NVFP4_API int nvfp4_experts_fp8_fwd(const void* X, int x_by_token, const void* W, int dtype, int64_t tokens, int64_t topk, int64_t experts,

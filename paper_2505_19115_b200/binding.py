@@ -133,9 +133,9 @@ def lib():
     L.nvfp4_quantize_fp8_experts.restype = ci
     L.nvfp4_quantize_fp8_experts.argtypes = [vp, ci, ci, i64, i64, i64, i64, i64, vp, vp, vp, ci, vp, vp, vp, vp, vp]
     L.nvfp4_gemm_fp8_experts.restype = ci
-    L.nvfp4_gemm_fp8_experts.argtypes = [vp, vp, vp, vp, i64, vp, i64, i64, i64, vp, ci, i64, vp]
+    L.nvfp4_gemm_fp8_experts.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, vp, i64, i64, vp, ci, i64, vp]
     L.nvfp4_gemm_fp8_experts_dw.restype = ci
-    L.nvfp4_gemm_fp8_experts_dw.argtypes = [vp, vp, vp, vp, i64, vp, i64, i64, i64, vp, ci, vp]
+    L.nvfp4_gemm_fp8_experts_dw.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, i64, i64, vp, ci, vp]
     L.nvfp4_experts_fp8_fwd.restype = ci
     L.nvfp4_experts_fp8_fwd.argtypes = [vp, ci, vp, ci, i64, i64, i64, i64, i64, vp, vp, vp, ci, vp, sz, vp]
     L.nvfp4_experts_fp8_bwd.restype = ci
@@ -730,7 +730,8 @@ def nvfp4_gemm_fp8_experts(a_codes, a_sf, b_codes, b_sf, plan, out_dtype=torch.f
     if out is None:
         out = torch.empty((R, N), dtype=out_dtype, device=a_codes.device)
     assert out.shape == (R, N) and out.stride(1) == 1
-    st = _native().nvfp4_gemm_fp8_experts(a_codes, a_sf, b_codes, b_sf, E, plan.offsets, R, N, K, out, out, out.stride(0), stream)
+    st = _native().nvfp4_gemm_fp8_experts(a_codes, a_sf, b_codes, b_sf, plan.tokens, plan.topk, E, plan.counts, plan.offsets, N, K, out, out,
+                                          out.stride(0), stream)
     _check(st, "nvfp4_gemm_fp8_experts")
     return out
 
@@ -742,7 +743,7 @@ def nvfp4_gemm_fp8_experts_dw(a_codes, a_sf, b_codes, b_sf, plan, out_dtype=torc
     if out is None:
         out = torch.empty((plan.experts, N, K), dtype=out_dtype, device=a_codes.device)
     assert out.shape == (plan.experts, N, K) and out.is_contiguous()
-    st = _native().nvfp4_gemm_fp8_experts_dw(a_codes, a_sf, b_codes, b_sf, plan.experts, plan.offsets, R, N, K, out, out, stream)
+    st = _native().nvfp4_gemm_fp8_experts_dw(a_codes, a_sf, b_codes, b_sf, plan.tokens, plan.topk, plan.experts, plan.offsets, N, K, out, out, stream)
     _check(st, "nvfp4_gemm_fp8_experts_dw")
     return out
 

@@ -74,9 +74,14 @@ struct Fp8Product {
   int64_t experts = 0;
   const int32_t* offsets = nullptr;
   bool by_rows = false;
+  const int32_t* counts = nullptr;      // by_rows: the rows of each segment that are no padding (null: unknown)
+  int64_t slots = 0;                    // by_rows: the sum of the counts, at most
 };
 int gemm_fp8(const Fp8Product& p, cudaStream_t s);
+// The same for few rows (gemm_fp8_few.cu): one product, or by rows with their counts.  Padding rows of D are not written.
+int gemm_fp8_few(const Fp8Product& p, cudaStream_t s);
 int fp8_error_word(unsigned int* out);
+int fp8_few_error_word(unsigned int* out);
 
 constexpr int64_t kMaxExperts = 1024;
 

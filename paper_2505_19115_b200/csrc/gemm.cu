@@ -1327,8 +1327,10 @@ extern "C" int nvfp4_device_error_word(uint32_t* host_out) {
   unsigned int tile_w = 0;
   if (int st = tile_error_word(&tile_w)) return st;
   w |= tile_w;
-  if (int st = fp8_error_word(&tile_w)) return st;
-  w |= tile_w;
+  for (auto word : {fp8_error_word, fp8_few_error_word}) {
+    if (int st = word(&tile_w)) return st;
+    w |= tile_w;
+  }
   *host_out = w;
   return NVFP4_OK;
 }

@@ -64,6 +64,9 @@ struct Params {
   int sfa_ktiles, sfb_ktiles;       // scale tiles along a row of them
   int a_row_tiles, b_row_tiles;     // row tiles of one matrix
   int d_is_bf16;
+  int ragged;                       // a row of D ends between two multiples of 16 bytes
+  void* out;                        // D, for that case
+  int64_t ldd;
 };
 
 // What a pair of CTAs computes at one time.
@@ -389,6 +392,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
 #pragma unroll
             for (int e = 0; e < 32; ++e) v[e] = r[c / 32][e];
           }
+          if (p.ragged && col0 + c + kChunkCols > p.N) {
+            // a tiled store clips at 16 bytes: where the rows of D end between, the last columns are stored one by one
+            const int row = row0 + lane, n = p.N - (col0 + c);
+            const int64_t at = ((GROUPS == 2 ? (int64_t)t.e * p.M : 0) + row) * p.ldd + col0 + c;
+            if (row < t.m_end && row < p.M) {
+#pragma unroll
+              for (int e = 0; e < kChunkCols; ++e) {
+                if (e >= n) break;
+                if constexpr (BF16_OUT) static_cast<uint16_t*>(p.out)[at + e] = (uint16_t)(v[e / 2] >> (16 * (e & 1)));
+                else static_cast<uint32_t*>(p.out)[at + e] = v[e];
+              }
+            }
+            break;
+          }
           if (lane == 0) tma_store_wait_read<0>();  // the chunk stored before this one has left the buffer
           __syncwarp();
 #pragma unroll
@@ -475,6 +492,7 @@ int launch(const Fp8Product& c, cudaStream_t s) {
   p.sfa_ktiles = p.sfb_ktiles = (int)ceil_div(fp8_blocks(c.K), 4);
   p.a_row_tiles = (int)ceil_div(c.M, 128); p.b_row_tiles = (int)ceil_div(c.N, 128);
   p.d_is_bf16 = c.d_dtype == NVFP4_BF16;
+  p.ragged = c.N * (p.d_is_bf16 ? 2 : 4) % 16 != 0; p.out = c.d; p.ldd = c.ldd;
   if (!codes_map(&p.a, c.a, c.M, c.K, 128) || !codes_map(&p.b, c.b, b_matrices * c.N, c.K, BN / 2) ||
       !scales_map(&p.sfa, c.a_sf, fp8_sf_tiles(c.M, c.K)) || !scales_map(&p.sfb, c.b_sf, b_matrices * fp8_sf_tiles(c.N, c.K)) ||
       !out_map(&p.d, c.d, d_matrices, c.M, c.N, c.ldd, p.d_is_bf16 != 0))
@@ -490,7 +508,14 @@ int launch(const Fp8Product& c, cudaStream_t s) {
 
 }  // namespace
 
+// Rows of A (of a segment, on average) up to which the product goes to gemm_fp8_few.cu: those that it takes at one time.  us, there / here:
+// 128 rows 11008 x 4096 13.7 / 15.9, 4096 x 11008 14.9 / 23.4, 4096 x 4096 10.3 / 11.3, 2816 x 1024 5.1 / 5.0; 64 experts of 2816 x 1024 with 8
+// rows each 34.5 / 47.6, 4 with 128 each 7.0 / 8.8.
+constexpr int64_t kFewRows = 128;
+
 int gemm_fp8(const Fp8Product& p, cudaStream_t s) {
+  if (!p.experts && p.M <= kFewRows) return gemm_fp8_few(p, s);
+  if (p.by_rows && p.counts && p.slots <= kFewRows * p.experts) return gemm_fp8_few(p, s);
   const int groups = p.experts == 0 ? 0 : p.by_rows ? 1 : 2;
   const bool narrow = groups == 2 ? p.N <= 128 : pair_tile_width(p.M, p.N) == 128;
   switch (groups) {
@@ -542,21 +567,25 @@ extern "C" int nvfp4_gemm_fp8(const uint8_t* a_codes, const uint8_t* a_sf, const
 }
 
 extern "C" int nvfp4_gemm_fp8_experts(const uint8_t* a_codes, const uint8_t* a_sf, const uint8_t* b_codes, const uint8_t* b_sf,
-                                      int64_t experts, const int32_t* offsets, int64_t rows, int64_t N, int64_t K,
-                                      void* d, int d_dtype, int64_t ldd, void* cuda_stream) {
+                                      int64_t tokens, int64_t topk, int64_t experts, const int32_t* counts, const int32_t* offsets,
+                                      int64_t N, int64_t K, void* d, int d_dtype, int64_t ldd, void* cuda_stream) {
+  const int64_t rows = nvfp4_expert_rows(tokens, topk, experts);
   if (int st = check_product(a_codes, a_sf, b_codes, b_sf, d, rows, N, K, d_dtype, ldd)) return st;
   if (int st = check_experts(experts, offsets, N, K)) return st;
-  if (rows % 128 != 0 || (ceil_div(rows, 256) + experts) * ceil_div(N, 128) > kMost) return NVFP4_ERR_SHAPE;
+  if (reinterpret_cast<uintptr_t>(counts) & 3u) return NVFP4_ERR_ALIGN;
+  if ((ceil_div(rows, 256) + experts) * ceil_div(N, 128) > kMost) return NVFP4_ERR_SHAPE;
   if (int st = check_arch()) return st;
-  return gemm_fp8({a_codes, a_sf, b_codes, b_sf, rows, N, K, d, d_dtype, ldd, experts, offsets, true}, static_cast<cudaStream_t>(cuda_stream));
+  return gemm_fp8({a_codes, a_sf, b_codes, b_sf, rows, N, K, d, d_dtype, ldd, experts, offsets, true, counts, tokens * topk},
+                  static_cast<cudaStream_t>(cuda_stream));
 }
 
 extern "C" int nvfp4_gemm_fp8_experts_dw(const uint8_t* a_codes, const uint8_t* a_sf, const uint8_t* b_codes, const uint8_t* b_sf,
-                                         int64_t experts, const int32_t* offsets, int64_t rows, int64_t N, int64_t K,
+                                         int64_t tokens, int64_t topk, int64_t experts, const int32_t* offsets, int64_t N, int64_t K,
                                          void* d, int d_dtype, void* cuda_stream) {
+  const int64_t rows = nvfp4_expert_rows(tokens, topk, experts);
   if (int st = check_product(a_codes, a_sf, b_codes, b_sf, d, N, K, rows, d_dtype, K)) return st;
   if (int st = check_experts(experts, offsets, N, K)) return st;
-  if (rows % 128 != 0 || experts * ceil_div(N, 256) * ceil_div(K, 128) > kMost) return NVFP4_ERR_SHAPE;
+  if (experts * ceil_div(N, 256) * ceil_div(K, 128) > kMost) return NVFP4_ERR_SHAPE;
   if (int st = check_arch()) return st;
   return gemm_fp8({a_codes, a_sf, b_codes, b_sf, N, K, rows, d, d_dtype, K, experts, offsets, false}, static_cast<cudaStream_t>(cuda_stream));
 }

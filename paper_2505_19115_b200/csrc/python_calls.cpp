@@ -146,7 +146,7 @@ PyObject* checked_call(int (*f)(A...), PyObject* const* args, Py_ssize_t n) {
   X(nvfp4_linear_bwd_bf16, 7, 9) X(nvfp4_linear_fwd_static, 2, 12)                                                          \
   X(nvfp4_quantize_fp8, 1) X(nvfp4_gemm_fp8, 8) X(nvfp4_linear_fp8_fwd, 2, 7) X(nvfp4_linear_fp8_bwd, 3, 8, 10)             \
   X(nvfp4_expert_sort) X(nvfp4_expert_gather, 1, 11) X(nvfp4_expert_combine, 1, 8) X(nvfp4_expert_combine_bwd, 1, 12)       \
-  X(nvfp4_quantize_fp8_experts, 1, 11) X(nvfp4_gemm_fp8_experts, 10) X(nvfp4_gemm_fp8_experts_dw, 10)                       \
+  X(nvfp4_quantize_fp8_experts, 1, 11) X(nvfp4_gemm_fp8_experts, 12) X(nvfp4_gemm_fp8_experts_dw, 11)                       \
   X(nvfp4_experts_fp8_fwd, 3, 12) X(nvfp4_experts_fp8_bwd, 3, 7, 16, 18)
 
 #define NVFP4_WRAPPER(name, ...)                                                       \

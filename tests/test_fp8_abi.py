@@ -63,12 +63,12 @@ def test_product_refusals():
     for status, changes in ((1, dict(a=None)), (1, dict(bsf=None)), (1, dict(d=None)), (4, dict(dtype=7)), (2, dict(M=0)), (2, dict(K=0)), (2, dict(ldd=4)),
                             (2, dict(M=BIG)), (2, dict(M=1 << 30, N=1 << 30, ldd=1 << 30)), (3, dict(a=ODD)), (3, dict(d=ODD)), (3, dict(ldd=10)), (3, dict(dtype=0, ldd=12))):
         _call("nvfp4_gemm_fp8", g, status, **changes)
-    g = dict(a=P, asf=P, b=P, bsf=P, E=4, offsets=P, rows_=256, N=8, K=100, d=P, dtype=1, ldd=8, stream=None)
-    for status, changes in ((1, dict(a=None)), (1, dict(offsets=None)), (4, dict(dtype=7)), (2, dict(E=0)), (2, dict(E=1025)), (2, dict(rows_=200)), (2, dict(rows_=0)),
-                            (2, dict(E=1024, N=1 << 22, ldd=1 << 22)), (3, dict(offsets=0x1002)), (3, dict(ldd=9))):
+    g = dict(a=P, asf=P, b=P, bsf=P, T=99, k=2, E=4, counts=P, offsets=P, N=8, K=100, d=P, dtype=1, ldd=8, stream=None)
+    for status, changes in ((1, dict(a=None)), (1, dict(offsets=None)), (4, dict(dtype=7)), (2, dict(E=0)), (2, dict(E=1025)), (2, dict(T=0)), (2, dict(k=-1)),
+                            (2, dict(E=1024, N=1 << 22, ldd=1 << 22)), (3, dict(offsets=0x1002)), (3, dict(counts=0x1002)), (3, dict(ldd=9))):
         _call("nvfp4_gemm_fp8_experts", g, status, **changes)
-    g = dict(a=P, asf=P, b=P, bsf=P, E=4, offsets=P, rows_=256, N=8, K=104, d=P, dtype=1, stream=None)
-    for status, changes in ((1, dict(b=None)), (1, dict(offsets=None)), (4, dict(dtype=7)), (2, dict(E=1025)), (2, dict(rows_=200)), (2, dict(N=0)), (3, dict(K=102)), (3, dict(d=ODD))):
+    g = dict(a=P, asf=P, b=P, bsf=P, T=99, k=2, E=4, offsets=P, N=8, K=104, d=P, dtype=1, stream=None)
+    for status, changes in ((1, dict(b=None)), (1, dict(offsets=None)), (4, dict(dtype=7)), (2, dict(E=1025)), (2, dict(T=0)), (2, dict(N=0)), (3, dict(K=102)), (3, dict(d=ODD))):
         _call("nvfp4_gemm_fp8_experts_dw", g, status, **changes)
 
 

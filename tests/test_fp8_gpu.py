@@ -262,3 +262,17 @@ def test_layer_of_the_350m_block_at_full_size():
     ref.assert_product(Y, *ref.product(ref.values(X), Wq), K)
     ref.assert_product(dX, *ref.product(ref.values(dY), Wq.T), N)
     ref.assert_product(dW, *ref.product(ref.values(dY.T), ref.values(X.T)), M)
+
+
+@pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M", [1, 2, 7, 8, 15, 16, 17, 31, 33, 63, 64, 65, 100, 127, 128, 129])
+def test_products_of_few_rows(M, out_dtype):
+    # tiles of B alone, shared by 2, 4 and 8 blocks along K, and more of them than multiprocessors
+    for N, K in ((20000, 264), (9000, 1000), (4104, 1000), (1000, 2056), (136, 4100), (5, 130)):
+        ops, a, b = _operands(M, N, K, M + N)
+        D = torch.full((M, -(-N // 8) * 8), 7.0, dtype=out_dtype, device="cuda")
+        nb.nvfp4_gemm_fp8(*ops, out=D[:, :N])
+        torch.cuda.synchronize()
+        assert nb.nvfp4_device_error_word() == 0
+        ref.assert_product(D[:, :N], *ref.product(a, b), K)
+        assert bool((D[:, N:] == 7).all())
