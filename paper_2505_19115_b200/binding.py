@@ -9,6 +9,7 @@ The calls that launch work go through the extension module _calls (csrc/python_c
 arguments), the queries through ctypes.
 """
 import ctypes as C
+import functools
 import os
 
 import torch
@@ -533,39 +534,30 @@ def nvfp4_sf_bytes_fp8(Rq: int, Kq: int, sf_layout: int = SF_SWIZZLED) -> int:
     return int(lib().nvfp4_sf_bytes_fp8(Rq, Kq, sf_layout))
 
 
-def _fp8_codes(lead, Rq, Kq, device):
-    """Codes [*lead, Rq, Kq], rows of a multiple of 16 bytes."""
-    return torch.empty((*lead, Rq, -(-Kq // 16) * 16), dtype=torch.uint8, device=device)[..., :Kq]
-
-
-def _fp8_outputs(lead, Rq, Kq, sf_layout, device):
-    if sf_layout == SF_LINEAR:
-        return _fp8_codes(lead, Rq, Kq, device), torch.empty((*lead, Rq, -(-Kq // 128)), dtype=torch.uint8, device=device)
-    n = (lead[0] if lead else 1) * (-(-Rq // 128)) * (-(-Kq // 512)) * 512
-    return _fp8_codes(lead, Rq, Kq, device), torch.empty(n, dtype=torch.uint8, device=device)
-
-
 def _fp8_operand(codes):
     """(matrices, Rq, Kq) of codes as the quantizer leaves them."""
-    lead, (Rq, Kq) = codes.shape[:-2], codes.shape[-2:]
+    shape, stride = codes.shape, codes.stride()
+    Rq, Kq = shape[-2:]
     pitch = -(-Kq // 16) * 16
-    if codes.element_size() != 1 or codes.stride(-1) != 1 or (Rq > 1 and codes.stride(-2) != pitch) or (
-            len(lead) == 1 and lead[0] > 1 and codes.stride(0) != Rq * pitch):
+    if codes.element_size() != 1 or stride[-1] != 1 or (Rq > 1 and stride[-2] != pitch) or (
+            len(shape) == 3 and shape[0] > 1 and stride[0] != Rq * pitch):
         raise ValueError("FP8 codes have one byte each and rows of a multiple of 16 bytes, one behind the other")
-    return lead[0] if lead else 1, Rq, Kq
+    return shape[0] if len(shape) == 3 else 1, Rq, Kq
 
 
 def nvfp4_quantize_fp8(x, block_rows: int = 1, row: bool = True, transposed: bool = False, sf_layout: int = SF_SWIZZLED, stream=None):
     """FP8 with a power-of-two scale for each block of 128 (block_rows 128: 128 x 128, for weights).  x [rows, cols], or dense
     [batch, rows, cols].  Returns (codes [..., rows, cols], scales, codes_t [..., cols, rows], scales_t), None for what is not wanted;
     scales: linear [..., Rq, ceil(Kq/128)], or a flat swizzled buffer."""
-    assert x.is_cuda and x.dim() in (2, 3) and x.stride(-1) == 1 and (x.dim() == 2 or x.is_contiguous())
-    lead, (rows, cols) = x.shape[:-2], x.shape[-2:]
-    out = (_fp8_outputs(lead, rows, cols, sf_layout, x.device) if row else (None, None)) + (
-        _fp8_outputs(lead, cols, rows, sf_layout, x.device) if transposed else (None, None))
+    shape, stride = x.shape, x.stride()
+    assert x.is_cuda and len(shape) in (2, 3) and stride[-1] == 1 and (len(shape) == 2 or x.is_contiguous())
+    rows, cols = shape[-2:]
+    batch = shape[0] if len(shape) == 3 else 0
+    native = _native()
+    out = native.empty_fp8(x, batch, rows, cols, int(row), int(transposed), sf_layout)
     # a matrix of one row has no leading dimension to speak of
-    ld = x.stride(-2) if rows > 1 else max(x.stride(-2), -(-cols // 8) * 8)
-    st = _native().nvfp4_quantize_fp8(x, x, lead[0] if lead else 1, rows, cols, ld, block_rows, *out, sf_layout, stream)
+    ld = stride[-2] if rows > 1 else max(stride[-2], -(-cols // 8) * 8)
+    st = native.nvfp4_quantize_fp8(x, x, batch or 1, rows, cols, ld, block_rows, *out, sf_layout, stream)
     _check(st, "nvfp4_quantize_fp8")
     return out
 
@@ -615,6 +607,7 @@ def nvfp4_linear_fp8_bwd(dY, W, X, dX=None, dW=None, dx_dtype=torch.float32, dw_
     return dX, dW
 
 
+@functools.lru_cache(maxsize=256)
 def nvfp4_expert_rows(tokens: int, topk: int, experts: int) -> int:
     return int(lib().nvfp4_expert_rows(tokens, topk, experts))
 
@@ -624,15 +617,13 @@ class ExpertPlan:
     slot_of [rows], int32 on the device."""
     __slots__ = ("tokens", "topk", "experts", "rows", "counts", "offsets", "row_of", "slot_of")
 
-    def __init__(self, tokens, topk, experts, device):
+    def __init__(self, tokens, topk, experts, like):
+        """Buffers on the device of the tensor `like`, not filled."""
         self.tokens, self.topk, self.experts = tokens, topk, experts
         self.rows = nvfp4_expert_rows(tokens, topk, experts)
         if self.rows == 0:
             raise NvFp4Error(2, "nvfp4_expert_rows")
-        self.counts = torch.empty(experts, dtype=torch.int32, device=device)
-        self.offsets = torch.empty(experts + 1, dtype=torch.int32, device=device)
-        self.row_of = torch.empty((tokens, topk), dtype=torch.int32, device=device)
-        self.slot_of = torch.empty(self.rows, dtype=torch.int32, device=device)
+        self.counts, self.offsets, self.row_of, self.slot_of = _native().expert_buffers(like, tokens, topk, experts, self.rows)
 
 
 def nvfp4_expert_sort(expert_of, experts: int, plan: ExpertPlan = None, stream=None) -> ExpertPlan:
@@ -642,7 +633,7 @@ def nvfp4_expert_sort(expert_of, experts: int, plan: ExpertPlan = None, stream=N
         raise TypeError(f"unsupported dtype {expert_of.dtype}")
     tokens, topk = expert_of.shape
     if plan is None:
-        plan = ExpertPlan(tokens, topk, experts, expert_of.device)
+        plan = ExpertPlan(tokens, topk, experts, expert_of)
     assert (plan.tokens, plan.topk, plan.experts) == (tokens, topk, experts)
     st = _native().nvfp4_expert_sort(expert_of, int(expert_of.dtype == torch.int64), tokens, topk, experts, plan.counts, plan.offsets,
                                      plan.row_of, plan.slot_of, stream)
@@ -663,7 +654,7 @@ def nvfp4_expert_gather(x, plan, weights=None, out=None, stream=None):
     assert x.dim() == 2 and x.stride(1) == 1 and x.shape[0] == plan.tokens
     cols = x.shape[1]
     if out is None:
-        out = torch.empty((plan.rows, cols), dtype=x.dtype, device=x.device)
+        out = _native().empty_rows(x, plan.rows, cols)
     assert out.is_contiguous() and out.shape == (plan.rows, cols) and out.dtype == x.dtype
     w, w_dtype = _weights(weights, plan)
     st = _native().nvfp4_expert_gather(x, x, plan.tokens, plan.topk, plan.experts, cols, x.stride(0) if plan.tokens > 1 else cols,
@@ -677,7 +668,7 @@ def nvfp4_expert_combine(rows, plan, weights=None, out=None, stream=None):
     assert rows.is_contiguous() and rows.dim() == 2 and rows.shape[0] == plan.rows
     cols = rows.shape[1]
     if out is None:
-        out = torch.empty((plan.tokens, cols), dtype=rows.dtype, device=rows.device)
+        out = _native().empty_rows(rows, plan.tokens, cols)
     assert out.is_contiguous() and out.shape == (plan.tokens, cols) and out.dtype == rows.dtype
     w, w_dtype = _weights(weights, plan)
     st = _native().nvfp4_expert_combine(rows, rows, plan.tokens, plan.topk, plan.experts, cols, plan.row_of, w, w_dtype, out, stream)
@@ -691,9 +682,9 @@ def nvfp4_expert_combine_bwd(dy, rows, plan, weights, rows_gradient: bool = True
     cols = dy.shape[1]
     assert rows.is_contiguous() and rows.shape == (plan.rows, cols)
     if drows is None and rows_gradient:
-        drows = torch.empty((plan.rows, cols), dtype=rows.dtype, device=rows.device)
+        drows = _native().empty_rows(rows, plan.rows, cols)
     if dweights is None:
-        dweights = torch.empty_like(weights)
+        dweights = _native().empty_rows(weights, plan.tokens, plan.topk)
     assert drows is None or (drows.is_contiguous() and drows.shape == rows.shape and drows.dtype == rows.dtype)
     assert weights.is_contiguous() and dweights.is_contiguous() and dweights.dtype == weights.dtype
     assert weights.shape == dweights.shape == (plan.tokens, plan.topk)
@@ -713,8 +704,7 @@ def nvfp4_quantize_fp8_experts(x, plan, weights=None, sorted_rows: bool = False,
     multiplied by weights.  Returns (codes [rows, cols], scales, codes_t [cols, rows], scales_t)."""
     by_token = _by_token(x, plan, sorted_rows)
     cols = x.shape[1]
-    out = (_fp8_outputs((), plan.rows, cols, SF_SWIZZLED, x.device) if row else (None, None)) + (
-        _fp8_outputs((), cols, plan.rows, SF_SWIZZLED, x.device) if transposed else (None, None))
+    out = _native().empty_fp8(x, 0, plan.rows, cols, int(row), int(transposed), SF_SWIZZLED)
     w, w_dtype = _weights(weights, plan)
     ld = x.stride(0) if x.shape[0] > 1 else max(x.stride(0), -(-cols // 8) * 8)
     st = _native().nvfp4_quantize_fp8_experts(x, x, by_token, plan.tokens, plan.topk, plan.experts, cols, ld, plan.offsets, plan.slot_of,
