@@ -76,6 +76,7 @@ struct Fp8Product {
   bool by_rows = false;
   const int32_t* counts = nullptr;      // by_rows: the rows of each segment that are no padding (null: unknown)
   int64_t slots = 0;                    // by_rows: the sum of the counts, at most
+  bool late = false;                    // nothing that it reads or writes is the kernel before's, and that one has waited for all before it
 };
 int gemm_fp8(const Fp8Product& p, cudaStream_t s);
 // The same for few rows (gemm_fp8_few.cu): one product, or by rows with their counts.  Padding rows of D are not written.

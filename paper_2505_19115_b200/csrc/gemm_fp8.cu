@@ -64,6 +64,7 @@ struct Params {
   int sfa_ktiles, sfb_ktiles;       // scale tiles along a row of them
   int a_row_tiles, b_row_tiles;     // row tiles of one matrix
   int d_is_bf16;
+  int late;                         // nothing that it reads or writes is the kernel before's (launch_overlapped)
   int ragged;                       // a row of D ends between two multiples of 16 bytes
   void* out;                        // D, for that case
   int64_t ldd;
@@ -167,7 +168,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
   if constexpr (GROUPS != 0) {
     // the segments' table, by one warp: a running sum of the tiles of 32 segments at a time
     if (warp == 2) {
-      grid_dependency_wait();
+      if (!p.late) grid_dependency_wait();
       int tiles = 0;
       for (int e0 = 0; e0 <= p.experts; e0 += 32) {
         const int e = e0 + lane;
@@ -192,8 +193,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
   cluster_sync_all();                               // both CTAs' barriers exist before any remote signal
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  // As in gemm.cu, each role waits for the kernel before this one directly before its first copy or bounded wait.
-  auto follow = [&] { grid_dependency_wait(); };
+  // As in gemm.cu, each role waits for the kernel before this one directly before its first copy or bounded wait; a late product waits
+  // at its end.
+  auto follow = [&] {
+    if (!p.late) grid_dependency_wait();
+  };
 
   if (warp < 8) {
     regs_release<kControlRegs>();
@@ -214,7 +218,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
           const uint32_t lead_full = map_to_cta(full_bar(s), 0);
           if (first) {
             follow();
-            grid_dependency_trigger();
+            if (!p.late) grid_dependency_trigger();
             first = false;
           }
           if (issuer) {
@@ -435,7 +439,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
     tc_fence_after();
     tmem_dealloc_pair(tmem_base, kTmemCols);
   }
-  grid_dependency_wait();                           // a pair without a tile has not waited: "finished" keeps meaning "and all before"
+  grid_dependency_wait();                           // a pair without a tile, or of a late product, has not waited: "finished" keeps meaning "and all before"
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -491,7 +495,7 @@ int launch(const Fp8Product& c, cudaStream_t s) {
   p.k_stages = (int)ceil_div(c.K, kBK); p.k_mmas = (int)ceil_div(c.K, 32);
   p.sfa_ktiles = p.sfb_ktiles = (int)ceil_div(fp8_blocks(c.K), 4);
   p.a_row_tiles = (int)ceil_div(c.M, 128); p.b_row_tiles = (int)ceil_div(c.N, 128);
-  p.d_is_bf16 = c.d_dtype == NVFP4_BF16;
+  p.d_is_bf16 = c.d_dtype == NVFP4_BF16; p.late = c.late;
   p.ragged = c.N * (p.d_is_bf16 ? 2 : 4) % 16 != 0; p.out = c.d; p.ldd = c.ldd;
   if (!codes_map(&p.a, c.a, c.M, c.K, 128) || !codes_map(&p.b, c.b, b_matrices * c.N, c.K, BN / 2) ||
       !scales_map(&p.sfa, c.a_sf, fp8_sf_tiles(c.M, c.K)) || !scales_map(&p.sfb, c.b_sf, b_matrices * fp8_sf_tiles(c.N, c.K)) ||

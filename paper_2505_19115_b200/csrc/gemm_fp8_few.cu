@@ -57,7 +57,7 @@ struct Params {
   int tokens, box;                  // a stage holds `tokens` rows of A (a multiple of 16), fetched `box` at a time
   int stages;
   int split;                        // blocks of a cluster
-  int d_is_bf16;
+  int d_is_bf16, late;
 };
 struct Item {
   int row, rows, n0, e;             // rows of A [row, row + rows), first column of D, matrix of B
@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp8_few_kernel(const __grid_
   if (warp == 1) tmem_alloc(smem_u32((const void*)tmem_slot), kTmemCols);
   if (warp == 2 && p.offsets) {
     // the segments' table: a running sum of the items of 32 segments at a time; what is no plan is cut to the rows that there are
-    grid_dependency_wait();
+    if (!p.late) grid_dependency_wait();
     int items = 0;
     for (int e0 = 0; e0 <= p.experts; e0 += 32) {
       const int e = e0 + lane;
@@ -167,7 +167,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp8_few_kernel(const __grid_
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  auto follow = [&] { grid_dependency_wait(); };
+  auto follow = [&] {                               // a late product waits at its end
+    if (!p.late) grid_dependency_wait();
+  };
 
   if (warp == 0) {
     // ------------------------------- operand producer -------------------------------
@@ -186,7 +188,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp8_few_kernel(const __grid_
         const uint32_t st = smem_base + s * stage_bytes;
         if (first) {
           follow();
-          grid_dependency_trigger();
+          if (!p.late) grid_dependency_trigger();
           first = false;
         }
         if (issuer) {
@@ -398,7 +400,7 @@ int gemm_fp8_few(const Fp8Product& c, cudaStream_t s) {
   Params p;
   const int64_t experts = c.experts ? c.experts : 1;
   p.offsets = c.experts ? c.offsets : nullptr; p.counts = c.counts;
-  p.d = c.d; p.ldd = c.ldd; p.d_is_bf16 = c.d_dtype == NVFP4_BF16;
+  p.d = c.d; p.ldd = c.ldd; p.d_is_bf16 = c.d_dtype == NVFP4_BF16; p.late = c.late;
   p.M = (int)c.M; p.N = (int)c.N; p.experts = (int)experts;
   p.tiles = (int)ceil_div(c.N, 128);
   p.slots = (int)c.slots;
