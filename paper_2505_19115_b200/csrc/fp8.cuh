@@ -58,7 +58,7 @@ struct Fp8Operand {
   Fp8Rows from;
 };
 constexpr int kMaxFp8Operands = 3;
-// One launch for all of them (quantize_fp8.cu); the caller has checked the arguments.
+// One launch for all of them, a second for those with weights (quantize_fp8.cu); the caller has checked the arguments.
 int quantize_fp8(const Fp8Operand* ops, int n, int dtype, int sf_layout, cudaStream_t s);
 
 // The products (gemm_fp8.cu); operands with swizzled scales.

@@ -360,3 +360,34 @@ def test_single_token_through_kept_weights():
             tol = sizes.sum(0) * (ref.accumulation(K) + (topk + 2) * 2.0 ** -24)
             assert bool(((y[t].double() - terms.sum(0)).abs() <= tol).all())
     assert nb.nvfp4_device_error_word() == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_weights_and_values_next_to_the_smallest_and_the_largest_numbers(dtype):
+    # a row's weight and its scale are one factor where that is exact; these are not, or are nearly not
+    T, topk, E, C = 40, 2, 3, 264
+    plan = nb.nvfp4_expert_sort(_choices(T, topk, E, 1, 0.0), E)
+    _, slot_of, used = _reference(plan)
+    source, pad = slot_of[:used].clamp(min=0), (slot_of[:used] < 0)[:, None]
+    x = _normal((T, C), 5, torch.float32)
+    x = (x * torch.exp2(torch.linspace(-126, 100, T, device="cuda"))[:, None]).to(dtype)
+    x[3], x[4, 5] = 0, float("nan")
+    for weights in (torch.exp2(torch.linspace(-20, 26, T * topk, device="cuda")) * 1.1, torch.full((T * topk,), 1e-38, device="cuda"),
+                    torch.full((T * topk,), -3e37, device="cuda"), torch.zeros(T * topk, device="cuda"), torch.full((T * topk,), float("inf"), device="cuda")):
+        w = weights.view(T, topk)
+        rows = torch.where(pad, 0, x[source // topk].float() * w.reshape(-1)[source][:, None])
+        codes, scales, codes_t, scales_t = nb.nvfp4_quantize_fp8_experts(x, plan, w, transposed=True)
+        for src, c, sf in ((rows, codes[:used], scales), (rows.T, codes_t[:, :used], scales_t)):
+            R, Cq = src.shape
+            bad = torch.nn.functional.pad(~src.isfinite(), (0, -Cq % 128)).view(R, -1, 128).any(2)
+            tiles = -(-(C if src is rows else plan.rows) // 512)
+            r, kb = torch.meshgrid(torch.arange(R, device="cuda"), torch.arange(bad.shape[1], device="cuda"), indexing="ij")
+            got = sf[((r // 128) * tiles + kb // 4) * 512 + (r % 32) * 16 + ((r % 128) // 32) * 4 + kb % 4]
+            assert torch.equal(got == 255, bad)
+            # a NaN or an infinity of a block hides its other values: those blocks are NaN, the others as defined
+            keep = ~bad.repeat_interleave(128, 1)[:, :Cq]
+            clean = torch.where(bad.repeat_interleave(128, 1)[:, :Cq], 0, src.nan_to_num(0, 0, 0))
+            y, e = ref.codes_and_exponents(clean)
+            assert torch.equal(c[keep], ref.code_bytes(y)[keep])
+            assert torch.equal(got[~bad], ref.scale_bytes(e)[~bad])
+            assert bool((c[~keep] & 127 == 127).all())
