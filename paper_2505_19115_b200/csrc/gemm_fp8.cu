@@ -6,8 +6,8 @@
 // the scales itself (the accumulator is never rescaled in registers); persistent, warp-specialised, roles and barriers as in the
 // NVFP4 pair kernel (gemm.cu): operands by tiled copies into a ring of k-stages of 128 values (128 bytes a row, 128-byte
 // swizzle), scales through registers into tensor memory, eight epilogue warps that move the accumulator out and store it by
-// tiled copies.  A stage is one block of the scales: a 512-byte scale tile (128 rows x 4 blocks) goes to tensor memory as it
-// is, four columns per 128 rows, and an instruction's descriptor names the byte of the column that is its stage's block.
+// tiled copies.  A stage is one block of the scales: a 512-byte scale tile (128 rows x 4 blocks) serves four stages; it goes to
+// tensor memory as it is, four columns per 128 rows, and an instruction's descriptor names the byte of the column that is its stage's block.
 //
 // One kernel, three forms (GROUPS):
 //   0  one product
@@ -40,18 +40,19 @@ struct Cfg {
   static constexpr int kBBytes = (BN / 2) * kBK;
   static constexpr int kSfbTiles = BN / 128;
   static constexpr int kSfBytes = (1 + kSfbTiles) * 512;
-  static constexpr int kStageBytes = kABytes + kBBytes + (kSfBytes + 1023) / 1024 * 1024;
+  static constexpr int kStageBytes = kABytes + kBBytes;
+  static constexpr int kSfSlots = 4;               // of scale tiles, each for up to four stages
   static constexpr int kEpiWarpBytes = 4096;       // a 32-row x 128-byte staging buffer per epilogue warp
   static constexpr int kEpiBytes = 8 * kEpiWarpBytes;
   static constexpr int kBarrierBytes = 512;
   static constexpr int kTableBytes = (kMaxExperts + 1) * 8 + 8;      // per segment: its first tile and its offset
-  static constexpr int kSmemBytes = kStages * kStageBytes + kEpiBytes + kBarrierBytes + kTableBytes + 1024 /*align*/;
-  // tensor memory: accumulators, then a buffer of 16 columns per stage (4 for A, 4 per 128 rows of B)
+  static constexpr int kSmemBytes = kStages * kStageBytes + kEpiBytes + kSfSlots * kSfBytes + kBarrierBytes + kTableBytes + 1024 /*align*/;
+  // tensor memory: accumulators, then 16 columns per slot of scales (4 for A, 4 per 128 rows of B)
   static constexpr uint32_t kSfCol = kAccStages * BN;
-  static constexpr int kNumBarriers = 5 * kStages + 2 * kAccStages;
+  static constexpr int kNumBarriers = 2 * kStages + 3 * kSfSlots + 2 * kAccStages;
   static_assert(kSmemBytes <= 232448, "shared memory overflow");
   static_assert(8 * kNumBarriers + 8 <= kBarrierBytes, "barrier area overflow");
-  static_assert(kSfCol + 16 * kStages <= kTmemCols, "tensor memory overflow");
+  static_assert(kSfCol + 16 * kSfSlots <= kTmemCols, "tensor memory overflow");
 };
 
 struct Params {
@@ -134,17 +135,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
   const uint32_t epi_base = smem_base + C::kStages * C::kStageBytes;
-  const uint32_t bar_base = epi_base + C::kEpiBytes;
-  uint8_t* bar_gen = smem_gen + C::kStages * C::kStageBytes + C::kEpiBytes;
-  // full: operands of both CTAs landed (leader's)     sfl: this CTA's scale tiles landed    empty: the stage's MMAs are done (both)
-  // sfr: the stage's scales are in tensor memory in both CTAs (leader's)   sfx: its scale tiles have been read out of shared memory
+  const uint32_t sf_base = epi_base + C::kEpiBytes, bar_base = sf_base + C::kSfSlots * C::kSfBytes;
+  uint8_t* sf_gen = smem_gen + C::kStages * C::kStageBytes + C::kEpiBytes;
+  uint8_t* bar_gen = sf_gen + C::kSfSlots * C::kSfBytes;
+  // full: operands of both CTAs landed (leader's)         empty: the stage's MMAs are done (both)
+  // sfl: this CTA's scale tiles landed   sfr: they are in tensor memory in both CTAs (leader's)   sfe: the MMAs of their stages are done (both)
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
-  auto sfl_bar = [&](int s) { return bar_base + 8u * (C::kStages + s); };
-  auto empty_bar = [&](int s) { return bar_base + 8u * (2 * C::kStages + s); };
-  auto sfr_bar = [&](int s) { return bar_base + 8u * (3 * C::kStages + s); };
-  auto sfx_bar = [&](int s) { return bar_base + 8u * (4 * C::kStages + s); };
-  auto tfull_bar = [&](int a) { return bar_base + 8u * (5 * C::kStages + a); };
-  auto tempty_bar = [&](int a) { return bar_base + 8u * (5 * C::kStages + C::kAccStages + a); };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (C::kStages + s); };
+  auto sfl_bar = [&](int q) { return bar_base + 8u * (2 * C::kStages + q); };
+  auto sfr_bar = [&](int q) { return bar_base + 8u * (2 * C::kStages + C::kSfSlots + q); };
+  auto sfe_bar = [&](int q) { return bar_base + 8u * (2 * C::kStages + 2 * C::kSfSlots + q); };
+  auto tfull_bar = [&](int a) { return bar_base + 8u * (2 * C::kStages + 3 * C::kSfSlots + a); };
+  auto tempty_bar = [&](int a) { return bar_base + 8u * (2 * C::kStages + 3 * C::kSfSlots + C::kAccStages + a); };
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(bar_gen + 8 * C::kNumBarriers);
   volatile uint32_t* abort_flag = tmem_slot + 1;
   int* const offsets = reinterpret_cast<int*>(bar_gen + C::kBarrierBytes);
@@ -155,9 +157,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
   const int pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < C::kStages; ++s) {
-      mbar_init(full_bar(s), 1); mbar_init(sfl_bar(s), 1); mbar_init(empty_bar(s), 1); mbar_init(sfr_bar(s), 8); mbar_init(sfx_bar(s), 4);
-    }
+    for (int s = 0; s < C::kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int q = 0; q < C::kSfSlots; ++q) { mbar_init(sfl_bar(q), 1); mbar_init(sfr_bar(q), 8); mbar_init(sfe_bar(q), 1); }
     for (int a = 0; a < C::kAccStages; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 16); }
     *abort_flag = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -236,7 +237,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
     } else if (warp == 2) {
       // ------------------------------- scale producer (both CTAs) -------------------------------
       const bool issuer = elect_one();
-      int s = 0;
+      int q = 0;
       uint32_t ph = 0;
       bool ok = true, first = true;
       Tile t;
@@ -246,19 +247,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
 #pragma unroll
         for (int h = 0; h < C::kSfbTiles; ++h)      // rows past N are never stored
           b_tile[h] = ((GROUPS == 1 ? t.e * p.b_row_tiles : 0) + min((t.n0 >> 7) + h, p.b_row_tiles - 1)) * p.sfb_ktiles;
-        for (int ks = 0; ks < t.stages; ++ks) {
-          ok = mbar_wait_relaxed(sfx_bar(s), ph ^ 1u, abort_flag, 0x48);
+        for (int kt = t.kb0 >> 2; kt < (t.kb0 + t.stages + 3) >> 2; ++kt) {
+          if (GROUPS == 2 && t.stages == 0) break;
+          ok = mbar_wait_relaxed(sfe_bar(q), ph ^ 1u, abort_flag, 0x48);
           if (!ok) break;
-          const uint32_t sf = smem_base + s * C::kStageBytes + C::kABytes + C::kBBytes;
+          const uint32_t sf = sf_base + q * C::kSfBytes;
           if (first) { follow(); first = false; }
           if (issuer) {
-            const int kt = (t.kb0 + ks) >> 2;
-            mbar_arrive_expect_tx(sfl_bar(s), C::kSfBytes);
-            tma_load_2d(sf, &p.sfa, sfl_bar(s), 0, a_tile + kt);
+            mbar_arrive_expect_tx(sfl_bar(q), C::kSfBytes);
+            tma_load_2d(sf, &p.sfa, sfl_bar(q), 0, a_tile + kt);
 #pragma unroll
-            for (int h = 0; h < C::kSfbTiles; ++h) tma_load_2d(sf + 512 + h * 512, &p.sfb, sfl_bar(s), 0, b_tile[h] + kt);
+            for (int h = 0; h < C::kSfbTiles; ++h) tma_load_2d(sf + 512 + h * 512, &p.sfb, sfl_bar(q), 0, b_tile[h] + kt);
           }
-          if (++s == C::kStages) { s = 0; ph ^= 1u; }
+          if (++q == C::kSfSlots) { q = 0; ph ^= 1u; }
         }
       }
       if (!ok && issuer) {
@@ -269,8 +270,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
       // ------------------------------- MMA issuer (leader CTA only) -------------------------------
       if (rank == 0) {
         const bool issuer = elect_one();
-        int s = 0, acc = 0;
-        uint32_t ph = 0, acc_ph = 0;
+        int s = 0, q = 0, acc = 0;
+        uint32_t ph = 0, q_ph = 0, acc_ph = 0;
         bool ok = true, first = true;
         Tile t;
         for (int item = pair; ok && tile_at<BN, GROUPS>(p, seg, item, t); item += num_pairs) {
@@ -279,13 +280,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
           if (!ok) break;
           const uint32_t d_tmem = tmem_base + acc * BN;
           for (int ks = 0; ks < t.stages; ++ks) {
-            ok = mbar_wait_issuer(full_bar(s), ph, abort_flag, 0x43) && mbar_wait_issuer(sfr_bar(s), ph, abort_flag, 0x45);
+            const uint32_t byte = (uint32_t)(t.kb0 + ks) & 3u;
+            const bool last_of_slot = byte == 3u || ks == t.stages - 1;
+            if (ks == 0 || byte == 0u) ok = mbar_wait_issuer(sfr_bar(q), q_ph, abort_flag, 0x45);
+            ok = ok && mbar_wait_issuer(full_bar(s), ph, abort_flag, 0x43);
             if (!ok) break;
             tc_fence_after();
             const uint32_t st = smem_base + s * C::kStageBytes;
-            const uint32_t byte = (uint32_t)(t.kb0 + ks) & 3u;
             const uint32_t idesc = instr_desc_mxf8(256, BN, 0) | byte << 4 | byte << 29;
-            const uint32_t sfa_t = tmem_base + C::kSfCol + s * 16, sfb_t = sfa_t + 4;
+            const uint32_t sfa_t = tmem_base + C::kSfCol + q * 16, sfb_t = sfa_t + 4;
             const uint64_t adesc = operand_desc(st), bdesc = operand_desc(st + C::kABytes);
             const int n = GROUPS == 2 ? 4 : min(4, p.k_mmas - ks * 4);
             if (issuer) {
@@ -295,8 +298,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
               } else {
                 for (int j = 0; j < n; ++j) tc_mma_mxf8_pair(d_tmem, adesc + 2u * j, bdesc + 2u * j, idesc, sfa_t, sfb_t, (ks | j) ? 1u : 0u);
               }
-              tc_commit_pair(empty_bar(s));         // shared memory and scale columns of the stage free in both CTAs
+              tc_commit_pair(empty_bar(s));         // the stage is free in both CTAs
+              if (last_of_slot) tc_commit_pair(sfe_bar(q));
             }
+            if (last_of_slot)
+              if (++q == C::kSfSlots) { q = 0; q_ph ^= 1u; }
             if (++s == C::kStages) { s = 0; ph ^= 1u; }
           }
           if (!ok) break;
@@ -310,18 +316,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
       // one column per group.
       const uint32_t lane_field = (uint32_t)((warp & 3) * 32) << 16;
       const uint32_t lead_sfr0 = map_to_cta(sfr_bar(0), 0);
-      int s = 0;
+      int q = 0;
       uint32_t ph = 0;
       bool ok = true, first = true;
       Tile t;
       for (int item = pair; ok && tile_at<BN, GROUPS>(p, seg, item, t); item += num_pairs) {
         if (first) { follow(); first = false; }
-        for (int ks = 0; ks < t.stages; ++ks) {
-          ok = mbar_wait_issuer(sfl_bar(s), ph, abort_flag, 0x46);
-          ok = ok && mbar_wait_issuer(empty_bar(s), ph ^ 1u, abort_flag, 0x47);
-          if (!(ok = warp_acquire(ok))) break;
+        for (int kt = t.kb0 >> 2; kt < (t.kb0 + t.stages + 3) >> 2; ++kt) {
+          if (GROUPS == 2 && t.stages == 0) break;
+          // the MMAs that read the slot's columns before are done: its copies were issued behind them
+          if (!(ok = warp_acquire(mbar_wait_issuer(sfl_bar(q), ph, abort_flag, 0x46)))) break;
           tc_fence_after();
-          const uint8_t* sf = smem_gen + s * C::kStageBytes + C::kABytes + C::kBBytes + lane * 16;
+          const uint8_t* sf = sf_gen + q * C::kSfBytes + lane * 16;
           uint32_t r[16];
 #pragma unroll
           for (int j = 0; j < 1 + C::kSfbTiles; ++j) {
@@ -330,14 +336,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
           }
 #pragma unroll
           for (int j = 4 * (1 + C::kSfbTiles); j < 16; ++j) r[j] = 0u;
-          tmem_st16(tmem_base + C::kSfCol + s * 16 + lane_field, r);
-          __syncwarp();
-          if (lane == 0) mbar_arrive(sfx_bar(s));   // the tiles are in registers: the slot may be refilled
+          tmem_st16(tmem_base + C::kSfCol + q * 16 + lane_field, r);
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(lead_sfr0 + 8u * s);
-          if (++s == C::kStages) { s = 0; ph ^= 1u; }
+          if (lane == 0) mbar_arrive_cluster(lead_sfr0 + 8u * q);
+          if (++q == C::kSfSlots) { q = 0; ph ^= 1u; }
         }
       }
     }
