@@ -28,21 +28,26 @@ namespace nvfp4 {
 namespace {
 
 constexpr int kThreads = 512;
-constexpr int kBK = 128;                           // values, and bytes of a row, per k-stage
+constexpr int kBK = 128;                           // values, and bytes of a row, per block of a k-stage
 constexpr uint32_t kTmemCols = 512;
 constexpr int kControlRegs = 72, kEpilogueRegs = 184;   // 256 x (72 + 184) = 65536, what the CTA is launched with
 
 template <int BN>
 struct Cfg {
-  static constexpr int kStages = BN == 256 ? 5 : 7;
+  // Blocks per k-stage.  The roles' hand-over of a stage takes about as long as a block's instructions of 128 columns, so that narrow
+  // tiles take two blocks at a time (us, one / two: 704 x 704 x 16384 35.0 / 30.3, 512 x 4096 x 11008 27.4 / 24.5); wide ones lose by it
+  // what the ring has in depth (16384 x 1024 x 2816 41.1 / 41.8).
+  static constexpr int kSub = BN == 256 ? 1 : 2;
+  static constexpr int kStages = BN == 256 ? 6 : 4;
   static constexpr int kAccStages = BN == 256 ? 1 : 2;
   static constexpr int kABytes = 128 * kBK;
   static constexpr int kBBytes = (BN / 2) * kBK;
   static constexpr int kSfbTiles = BN / 128;
   static constexpr int kSfBytes = (1 + kSfbTiles) * 512;
-  static constexpr int kStageBytes = kABytes + kBBytes;
+  static constexpr int kBlockBytes = kABytes + kBBytes;
+  static constexpr int kStageBytes = kSub * kBlockBytes;
   static constexpr int kSfSlots = 4;               // of scale tiles, each for up to four stages
-  static constexpr int kEpiWarpBytes = 4096;       // a 32-row x 128-byte staging buffer per epilogue warp
+  static constexpr int kEpiWarpBytes = 2048;       // a 32-row x 64-byte staging buffer per epilogue warp
   static constexpr int kEpiBytes = 8 * kEpiWarpBytes;
   static constexpr int kBarrierBytes = 512;
   static constexpr int kTableBytes = (kMaxExperts + 1) * 8 + 8;      // per segment: its first tile and its offset
@@ -61,7 +66,7 @@ struct Params {
   int experts, rows;                // rows: of all segments, at most
   int M, N;                         // GROUPS == 1: M = all rows
   int tiles_m, tiles_n;             // GROUPS == 1: tiles_m comes from the offsets
-  int k_stages, k_mmas;             // GROUPS == 2: from the offsets
+  int k_blocks, k_mmas;             // GROUPS == 2: from the offsets
   int sfa_ktiles, sfb_ktiles;       // scale tiles along a row of them
   int a_row_tiles, b_row_tiles;     // row tiles of one matrix
   int d_is_bf16;
@@ -75,7 +80,7 @@ struct Params {
 struct Tile {
   int m0, n0;                       // first row of A and of D, first row of B within its matrix = first column of D
   int e;                            // matrix of B (GROUPS 1) or of D (GROUPS 2)
-  int kb0, stages;                  // first block along the contraction axis, k-stages
+  int kb0, blocks;                  // first block along the contraction axis, and how many
   int m_end;                        // rows from here on are not stored
 };
 
@@ -100,7 +105,7 @@ __device__ __forceinline__ bool tile_at(const Params& p, const Segments& seg, in
   if constexpr (GROUPS == 0) {
     if (item >= p.tiles_m * p.tiles_n) return false;
     tile_coords(item, p.tiles_m, p.tiles_n, tm, tn);
-    t.e = 0; t.kb0 = 0; t.stages = p.k_stages; t.m_end = p.M;
+    t.e = 0; t.kb0 = 0; t.blocks = p.k_blocks; t.m_end = p.M;
     t.m0 = tm * 256;
   } else if constexpr (GROUPS == 1) {
     if (item >= seg.firsts[p.experts]) return false;
@@ -113,7 +118,7 @@ __device__ __forceinline__ bool tile_at(const Params& p, const Segments& seg, in
     const int begin = seg.offsets[lo];
     t.m_end = seg.offsets[lo + 1];
     tile_coords(item - seg.firsts[lo], (t.m_end - begin + 255) >> 8, p.tiles_n, tm, tn);   // a segment with a tile has rows
-    t.kb0 = 0; t.stages = p.k_stages;
+    t.kb0 = 0; t.blocks = p.k_blocks;
     t.m0 = begin + tm * 256;
   } else {
     const int per = p.tiles_m * p.tiles_n;
@@ -121,7 +126,7 @@ __device__ __forceinline__ bool tile_at(const Params& p, const Segments& seg, in
     t.e = item / per;
     tile_coords(item - t.e * per, p.tiles_m, p.tiles_n, tm, tn);
     t.kb0 = seg.offsets[t.e] >> 7;
-    t.stages = max((seg.offsets[t.e + 1] >> 7) - t.kb0, 0);
+    t.blocks = max((seg.offsets[t.e + 1] >> 7) - t.kb0, 0);
     t.m0 = tm * 256; t.m_end = p.M;
   }
   t.n0 = tn * BN;
@@ -212,7 +217,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
       for (int item = pair; ok && tile_at<BN, GROUPS>(p, seg, item, t); item += num_pairs) {
         const int a_row = t.m0 + (int)rank * 128;
         const int b_row = (GROUPS == 1 ? t.e * p.N : 0) + t.n0 + (int)rank * (BN / 2);
-        for (int ks = 0; ks < t.stages; ++ks) {
+        for (int kb = 0; kb < t.blocks; kb += C::kSub) {
           ok = mbar_wait_issuer(empty_bar(s), ph ^ 1u, abort_flag, 0x41);
           if (!ok) break;
           const uint32_t st = smem_base + s * C::kStageBytes;
@@ -223,9 +228,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
             first = false;
           }
           if (issuer) {
-            if (rank == 0) mbar_arrive_expect_tx(full_bar(s), 2u * (C::kABytes + C::kBBytes));   // of both CTAs
-            tma_load_2d_pair(st, &p.a, lead_full, (t.kb0 + ks) * kBK, a_row);
-            tma_load_2d_pair(st + C::kABytes, &p.b, lead_full, (t.kb0 + ks) * kBK, b_row);
+            const int n = min(C::kSub, t.blocks - kb);
+            if (rank == 0) mbar_arrive_expect_tx(full_bar(s), 2u * C::kBlockBytes * n);   // of both CTAs
+#pragma unroll
+            for (int u = 0; u < C::kSub; ++u) {
+              if (u >= n) break;
+              tma_load_2d_pair(st + u * C::kBlockBytes, &p.a, lead_full, (t.kb0 + kb + u) * kBK, a_row);
+              tma_load_2d_pair(st + u * C::kBlockBytes + C::kABytes, &p.b, lead_full, (t.kb0 + kb + u) * kBK, b_row);
+            }
           }
           if (++s == C::kStages) { s = 0; ph ^= 1u; }
         }
@@ -247,8 +257,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
 #pragma unroll
         for (int h = 0; h < C::kSfbTiles; ++h)      // rows past N are never stored
           b_tile[h] = ((GROUPS == 1 ? t.e * p.b_row_tiles : 0) + min((t.n0 >> 7) + h, p.b_row_tiles - 1)) * p.sfb_ktiles;
-        for (int kt = t.kb0 >> 2; kt < (t.kb0 + t.stages + 3) >> 2; ++kt) {
-          if (GROUPS == 2 && t.stages == 0) break;
+        for (int kt = t.kb0 >> 2; kt < (t.kb0 + t.blocks + 3) >> 2; ++kt) {
+          if (GROUPS == 2 && t.blocks == 0) break;
           ok = mbar_wait_relaxed(sfe_bar(q), ph ^ 1u, abort_flag, 0x48);
           if (!ok) break;
           const uint32_t sf = sf_base + q * C::kSfBytes;
@@ -279,30 +289,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
           ok = mbar_wait_issuer(tempty_bar(acc), acc_ph ^ 1u, abort_flag, 0x42);
           if (!ok) break;
           const uint32_t d_tmem = tmem_base + acc * BN;
-          for (int ks = 0; ks < t.stages; ++ks) {
-            const uint32_t byte = (uint32_t)(t.kb0 + ks) & 3u;
-            const bool last_of_slot = byte == 3u || ks == t.stages - 1;
-            if (ks == 0 || byte == 0u) ok = mbar_wait_issuer(sfr_bar(q), q_ph, abort_flag, 0x45);
-            ok = ok && mbar_wait_issuer(full_bar(s), ph, abort_flag, 0x43);
+          for (int kb = 0; kb < t.blocks; kb += C::kSub) {
+            ok = mbar_wait_issuer(full_bar(s), ph, abort_flag, 0x43);
             if (!ok) break;
-            tc_fence_after();
             const uint32_t st = smem_base + s * C::kStageBytes;
-            const uint32_t idesc = instr_desc_mxf8(256, BN, 0) | byte << 4 | byte << 29;
-            const uint32_t sfa_t = tmem_base + C::kSfCol + q * 16, sfb_t = sfa_t + 4;
-            const uint64_t adesc = operand_desc(st), bdesc = operand_desc(st + C::kABytes);
-            const int n = GROUPS == 2 ? 4 : min(4, p.k_mmas - ks * 4);
-            if (issuer) {
-              if (n == 4) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) tc_mma_mxf8_pair(d_tmem, adesc + 2u * j, bdesc + 2u * j, idesc, sfa_t, sfb_t, (ks | j) ? 1u : 0u);
-              } else {
-                for (int j = 0; j < n; ++j) tc_mma_mxf8_pair(d_tmem, adesc + 2u * j, bdesc + 2u * j, idesc, sfa_t, sfb_t, (ks | j) ? 1u : 0u);
+            for (int u = 0; u < C::kSub; ++u) {
+              if (kb + u >= t.blocks) break;
+              const uint32_t byte = (uint32_t)(t.kb0 + kb + u) & 3u;
+              if (kb + u == 0 || byte == 0u) ok = mbar_wait_issuer(sfr_bar(q), q_ph, abort_flag, 0x45);
+              if (!ok) break;
+              tc_fence_after();
+              const uint32_t idesc = instr_desc_mxf8(256, BN, 0) | byte << 4 | byte << 29;
+              const uint32_t sfa_t = tmem_base + C::kSfCol + q * 16, sfb_t = sfa_t + 4;
+              const uint64_t adesc = operand_desc(st + u * C::kBlockBytes), bdesc = operand_desc(st + u * C::kBlockBytes + C::kABytes);
+              const int n = GROUPS == 2 ? 4 : min(4, p.k_mmas - (kb + u) * 4);
+              const bool last_of_slot = byte == 3u || kb + u == t.blocks - 1;
+              if (issuer) {
+                if (n == 4) {
+#pragma unroll
+                  for (int j = 0; j < 4; ++j) tc_mma_mxf8_pair(d_tmem, adesc + 2u * j, bdesc + 2u * j, idesc, sfa_t, sfb_t, (kb | u | j) ? 1u : 0u);
+                } else {
+                  for (int j = 0; j < n; ++j) tc_mma_mxf8_pair(d_tmem, adesc + 2u * j, bdesc + 2u * j, idesc, sfa_t, sfb_t, (kb | u | j) ? 1u : 0u);
+                }
+                if (last_of_slot) tc_commit_pair(sfe_bar(q));
               }
-              tc_commit_pair(empty_bar(s));         // the stage is free in both CTAs
-              if (last_of_slot) tc_commit_pair(sfe_bar(q));
+              if (last_of_slot)
+                if (++q == C::kSfSlots) { q = 0; q_ph ^= 1u; }
             }
-            if (last_of_slot)
-              if (++q == C::kSfSlots) { q = 0; q_ph ^= 1u; }
+            if (!ok) break;
+            if (issuer) tc_commit_pair(empty_bar(s));   // the stage is free in both CTAs
             if (++s == C::kStages) { s = 0; ph ^= 1u; }
           }
           if (!ok) break;
@@ -322,8 +338,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
       Tile t;
       for (int item = pair; ok && tile_at<BN, GROUPS>(p, seg, item, t); item += num_pairs) {
         if (first) { follow(); first = false; }
-        for (int kt = t.kb0 >> 2; kt < (t.kb0 + t.stages + 3) >> 2; ++kt) {
-          if (GROUPS == 2 && t.stages == 0) break;
+        for (int kt = t.kb0 >> 2; kt < (t.kb0 + t.blocks + 3) >> 2; ++kt) {
+          if (GROUPS == 2 && t.blocks == 0) break;
           // the MMAs that read the slot's columns before are done: its copies were issued behind them
           if (!(ok = warp_acquire(mbar_wait_issuer(sfl_bar(q), ph, abort_flag, 0x46)))) break;
           tc_fence_after();
@@ -374,7 +390,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(lead_tempty0 + 8u * acc);   // accumulator fully read: hand it back to the leader
       if (++acc == C::kAccStages) { acc = 0; acc_ph ^= 1u; }
-      if (GROUPS == 2 && t.stages == 0) {            // an empty segment: nothing was accumulated
+      if (GROUPS == 2 && t.blocks == 0) {            // an empty segment: nothing was accumulated
 #pragma unroll
         for (int l = 0; l < kLoads; ++l)
 #pragma unroll
@@ -384,21 +400,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
       if (row0 >= t.m_end) continue;                 // rows of the next segment, or past the last
       auto store_chunks = [&](auto bf16) {
         constexpr bool BF16_OUT = decltype(bf16)::value;
-        constexpr int kChunkCols = BF16_OUT ? 64 : 32;             // accumulator columns per 128 bytes of output row
+        constexpr int kChunkCols = BF16_OUT ? 32 : 16;             // accumulator columns per 64 bytes of output row
 #pragma unroll
         for (int c = 0; c < kWarpCols; c += kChunkCols) {
           if (col0 + c >= p.N) break;
-          uint32_t v[32];
+          uint32_t v[16];
           if constexpr (BF16_OUT) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
+            for (int e = 0; e < 16; ++e) {
               const uint32_t* x = r[(c + 2 * e) / 32] + (2 * e) % 32;
               const __nv_bfloat162 h2 = __floats2bfloat162_rn(__uint_as_float(x[0]), __uint_as_float(x[1]));
               v[e] = *reinterpret_cast<const uint32_t*>(&h2);
             }
           } else {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) v[e] = r[c / 32][e];
+            for (int e = 0; e < 16; ++e) v[e] = r[c / 32][c % 32 + e];
           }
           if (p.ragged && col0 + c + kChunkCols > p.N) {
             // a tiled store clips at 16 bytes: where the rows of D end between, the last columns are stored one by one
@@ -417,8 +433,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
           if (lane == 0) tma_store_wait_read<0>();  // the chunk stored before this one has left the buffer
           __syncwarp();
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {              // row = lane, 16-byte pieces, piece XOR (row & 7): the 128-byte swizzle
-            const uint32_t dst = buf + lane * 128 + ((e ^ (lane & 7)) << 4);
+          for (int e = 0; e < 4; ++e) {              // row = lane, 16-byte pieces, piece XOR bits 7-8 of the row's offset: the 64-byte swizzle
+            const uint32_t dst = buf + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4);
             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v[4 * e]), "r"(v[4 * e + 1]),
                          "r"(v[4 * e + 2]), "r"(v[4 * e + 3]) : "memory");
           }
@@ -471,17 +487,17 @@ bool scales_map(CUtensorMap* map, const uint8_t* base, int64_t tiles) {
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<uint8_t*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// Output [matrices, rows, cols] -> boxes of 32 rows x 128 bytes of one matrix.
+// Output [matrices, rows, cols] -> boxes of 32 rows x 64 bytes of one matrix.
 bool out_map(CUtensorMap* map, void* base, int64_t matrices, int64_t rows, int64_t cols, int64_t ldd, bool bf16) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (!fn) return false;
   const cuuint64_t esz = bf16 ? 2 : 4;
   const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)matrices};
   const cuuint64_t strides[2] = {(cuuint64_t)ldd * esz, (cuuint64_t)(rows * ldd) * esz};
-  const cuuint32_t box[3] = {(cuuint32_t)(128 / esz), 32, 1};
+  const cuuint32_t box[3] = {(cuuint32_t)(64 / esz), 32, 1};
   const cuuint32_t estr[3] = {1, 1, 1};
   return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, base, dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -496,7 +512,7 @@ int launch(const Fp8Product& c, cudaStream_t s) {
   p.rows = (int)(GROUPS == 1 ? c.M : c.K);
   p.M = (int)c.M; p.N = (int)c.N;
   p.tiles_m = (int)ceil_div(c.M, 256); p.tiles_n = (int)ceil_div(c.N, BN);
-  p.k_stages = (int)ceil_div(c.K, kBK); p.k_mmas = (int)ceil_div(c.K, 32);
+  p.k_blocks = (int)ceil_div(c.K, kBK); p.k_mmas = (int)ceil_div(c.K, 32);
   p.sfa_ktiles = p.sfb_ktiles = (int)ceil_div(fp8_blocks(c.K), 4);
   p.a_row_tiles = (int)ceil_div(c.M, 128); p.b_row_tiles = (int)ceil_div(c.N, 128);
   p.d_is_bf16 = c.d_dtype == NVFP4_BF16; p.late = c.late;
