@@ -93,6 +93,28 @@ __device__ __forceinline__ void tile_coords(int tile, int tiles_m, int tiles_n, 
   tm = panel * kPanel + in_panel - tn * height;
 }
 
+// The tensor core adds to its accumulator with truncation, so that an error grows with the number of additions: on normal values
+// 7e-7 of the result at a contraction of 11008, over 1e-6 at 16384 (a sum in fp32 rounded at every step: 2e-7).  Contractions longer than
+// kMostBlocks blocks are summed in equal parts, which the epilogue adds up in registers (LONG: a kernel of their own, since the others lose
+// 2 % by the choice).  A part costs a turn-round of the accumulator.
+constexpr int kMostBlocks = 96;
+template <bool LONG>
+__device__ __forceinline__ int part_blocks(int blocks, int sub) {
+  if (!LONG || blocks <= kMostBlocks) return blocks;
+  const int parts = (blocks + kMostBlocks - 1) / kMostBlocks;
+  return ((blocks + parts - 1) / parts + sub - 1) / sub * sub;
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr) : "memory");
+  tmem_ld_wait();
+#pragma unroll
+  for (int i = 0; i < 16; i += 4) asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3])::"memory");
+}
+
 // The table of segments in shared memory: firsts[e] the first tile of segment e, offsets[e] its first row.
 struct Segments {
   const int* firsts;
@@ -133,7 +155,7 @@ __device__ __forceinline__ bool tile_at(const Params& p, const Segments& seg, in
   return true;
 }
 
-template <int BN, int GROUPS>
+template <int BN, int GROUPS, bool LONG>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp8_kernel(const __grid_constant__ Params p) {
   using C = Cfg<BN>;
   extern __shared__ uint8_t smem_raw[];
@@ -288,8 +310,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
           if (first) { follow(); first = false; }
           ok = mbar_wait_issuer(tempty_bar(acc), acc_ph ^ 1u, abort_flag, 0x42);
           if (!ok) break;
-          const uint32_t d_tmem = tmem_base + acc * BN;
+          const int part = part_blocks<LONG>(t.blocks, C::kSub);
+          int begin = 0;                            // of the part
           for (int kb = 0; kb < t.blocks; kb += C::kSub) {
+            if (LONG && kb == begin + part) {
+              begin = kb;
+              if (issuer) tc_commit_pair(tfull_bar(acc));
+              if (++acc == C::kAccStages) { acc = 0; acc_ph ^= 1u; }
+              ok = mbar_wait_issuer(tempty_bar(acc), acc_ph ^ 1u, abort_flag, 0x42);
+              if (!ok) break;
+            }
+            const uint32_t d_tmem = tmem_base + acc * BN;
             ok = mbar_wait_issuer(full_bar(s), ph, abort_flag, 0x43);
             if (!ok) break;
             const uint32_t st = smem_base + s * C::kStageBytes;
@@ -308,9 +339,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
               if (issuer) {
                 if (n == 4) {
 #pragma unroll
-                  for (int j = 0; j < 4; ++j) tc_mma_mxf8_pair(d_tmem, adesc + 2u * j, bdesc + 2u * j, idesc, sfa_t, sfb_t, (kb | u | j) ? 1u : 0u);
+                  for (int j = 0; j < 4; ++j) tc_mma_mxf8_pair(d_tmem, adesc + 2u * j, bdesc + 2u * j, idesc, sfa_t, sfb_t, (kb > begin || u || j) ? 1u : 0u);
                 } else {
-                  for (int j = 0; j < n; ++j) tc_mma_mxf8_pair(d_tmem, adesc + 2u * j, bdesc + 2u * j, idesc, sfa_t, sfb_t, (kb | u | j) ? 1u : 0u);
+                  for (int j = 0; j < n; ++j) tc_mma_mxf8_pair(d_tmem, adesc + 2u * j, bdesc + 2u * j, idesc, sfa_t, sfb_t, (kb > begin || u || j) ? 1u : 0u);
                 }
                 if (last_of_slot) tc_commit_pair(sfe_bar(q));
               }
@@ -376,20 +407,45 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
     Tile t;
     for (int item = pair; ok && tile_at<BN, GROUPS>(p, seg, item, t); item += num_pairs) {
       if (first) { follow(); first = false; }
-      ok = mbar_wait_warp_spin(tfull_bar(acc), acc_ph, abort_flag, 0x44);
+      auto begin_part = [&] {                        // the address of this warp's share of the finished accumulator
+        ok = mbar_wait_warp_spin(tfull_bar(acc), acc_ph, abort_flag, 0x44);
+        tc_fence_after();
+        return tmem_base + acc * BN + half * kWarpCols + ((uint32_t)(quarter * 32) << 16);
+      };
+      auto end_part = [&] {                          // accumulator fully read: hand it back to the leader
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(lead_tempty0 + 8u * acc);
+        if (++acc == C::kAccStages) { acc = 0; acc_ph ^= 1u; }
+      };
+      uint32_t t_row = begin_part();
       if (!ok) break;
-      tc_fence_after();
       uint32_t r[kLoads][32];
-      const uint32_t t_row = tmem_base + acc * BN + half * kWarpCols + ((uint32_t)(quarter * 32) << 16);
 #pragma unroll
       for (int l = 0; l < kLoads; ++l) tmem_ld32(t_row + 32 * l, r[l]);
       tmem_ld_wait();
 #pragma unroll
       for (int l = 0; l < kLoads; ++l) tmem_ld_pin(r[l]);
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(lead_tempty0 + 8u * acc);   // accumulator fully read: hand it back to the leader
-      if (++acc == C::kAccStages) { acc = 0; acc_ph ^= 1u; }
+      end_part();
+      if constexpr (LONG) {
+        const int part = part_blocks<LONG>(t.blocks, C::kSub);
+        for (int kb = part; kb < t.blocks; kb += part) {
+          t_row = begin_part();
+          if (!ok) break;
+#pragma unroll
+          for (int l = 0; l < 2 * kLoads; ++l) {
+            uint32_t more[16];
+            tmem_ld16(t_row + 16 * l, more);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              uint32_t& sum = r[l / 2][16 * (l & 1) + e];
+              sum = __float_as_uint(__uint_as_float(sum) + __uint_as_float(more[e]));
+            }
+          }
+          end_part();
+        }
+        if (!ok) break;
+      }
       if (GROUPS == 2 && t.blocks == 0) {            // an empty segment: nothing was accumulated
 #pragma unroll
         for (int l = 0; l < kLoads; ++l)
@@ -501,7 +557,7 @@ bool out_map(CUtensorMap* map, void* base, int64_t matrices, int64_t rows, int64
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int BN, int GROUPS>
+template <int BN, int GROUPS, bool LONG>
 int launch(const Fp8Product& c, cudaStream_t s) {
   using C = Cfg<BN>;
   Params p;
@@ -525,9 +581,14 @@ int launch(const Fp8Product& c, cudaStream_t s) {
   const int64_t tiles = GROUPS == 1 ? (ceil_div(c.M, 256) + experts) * p.tiles_n : d_matrices * p.tiles_m * (int64_t)p.tiles_n;
   const int64_t pairs = std::min<int64_t>(tiles, sm_count() / 2);
   static DeviceFlags smem_set;                         // per instantiation, per device
-  if (set_max_dynamic_smem(smem_set, gemm_fp8_kernel<BN, GROUPS>, C::kSmemBytes) != cudaSuccess) return NVFP4_ERR_CUDA;
-  return launch_overlapped(gemm_fp8_kernel<BN, GROUPS>, (unsigned)(2 * pairs), kThreads, C::kSmemBytes, s, p) == cudaSuccess ? NVFP4_OK
+  if (set_max_dynamic_smem(smem_set, gemm_fp8_kernel<BN, GROUPS, LONG>, C::kSmemBytes) != cudaSuccess) return NVFP4_ERR_CUDA;
+  return launch_overlapped(gemm_fp8_kernel<BN, GROUPS, LONG>, (unsigned)(2 * pairs), kThreads, C::kSmemBytes, s, p) == cudaSuccess ? NVFP4_OK
                                                                                                                             : NVFP4_ERR_CUDA;
+}
+
+template <int BN, int GROUPS>
+int launch(const Fp8Product& c, cudaStream_t s) {
+  return fp8_blocks(c.K) > kMostBlocks ? launch<BN, GROUPS, true>(c, s) : launch<BN, GROUPS, false>(c, s);
 }
 
 }  // namespace

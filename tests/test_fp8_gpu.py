@@ -264,6 +264,17 @@ def test_layer_of_the_350m_block_at_full_size():
     ref.assert_product(dW, *ref.product(ref.values(dY.T), ref.values(X.T)), M)
 
 
+@pytest.mark.parametrize("K", [12288, 12289, 12416, 12680, 16384, 24600, 40000])
+@pytest.mark.parametrize("M,N", [(300, 600), (200, 5000), (3000, 3008)])
+def test_long_contractions_are_summed_in_parts(M, N, K):
+    ops, a, b = _operands(M, N, K, K)
+    D = nb.nvfp4_gemm_fp8(*ops)
+    torch.cuda.synchronize()
+    assert nb.nvfp4_device_error_word() == 0
+    # additions in the tensor core: those of the longest part, at most 96 blocks; then one for each part
+    ref.assert_product(D, *ref.product(a, b), 96 * 128 + 32 * (K // 12288 + 1))
+
+
 @pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("M", [1, 2, 7, 8, 15, 16, 17, 31, 33, 63, 64, 65, 100, 127, 128, 129])
 def test_products_of_few_rows(M, out_dtype):
