@@ -85,8 +85,6 @@ struct GemmCall {
   int d_dtype;
   int64_t ldd;
 };
-// Columns of the CTA-pair kernel's tiles for a product (gemm.cu): 128 or 256.
-int pair_tile_width(int64_t M, int64_t N);
 // Two products that do not depend on one another, in one launch; and the two of nvfp4_linear_bwd_bf16 (gemm.cu).
 int gemm_two(const GemmCall& x, const GemmCall& y, void* cuda_stream);
 int gemm_bf16_gradients(const void* dY, const void* W, const void* X, int64_t M, int64_t N, int64_t K, void* dX, int dx_dtype,

@@ -37,12 +37,12 @@ struct Cfg {
   // Blocks per k-stage.  The roles' hand-over of a stage takes about as long as a block's instructions of 128 columns, so that narrow
   // tiles take two blocks at a time (us, one / two: 704 x 704 x 16384 35.0 / 30.3, 512 x 4096 x 11008 27.4 / 24.5); wide ones lose by it
   // what the ring has in depth (16384 x 1024 x 2816 41.1 / 41.8).
-  static constexpr int kSub = BN == 256 ? 1 : 2;
-  static constexpr int kStages = BN == 256 ? 6 : 4;
+  static constexpr int kSub = BN == 128 ? 2 : 1;
+  static constexpr int kStages = BN == 128 ? 4 : 6;
   static constexpr int kAccStages = BN == 256 ? 1 : 2;
   static constexpr int kABytes = 128 * kBK;
   static constexpr int kBBytes = (BN / 2) * kBK;
-  static constexpr int kSfbTiles = BN / 128;
+  static constexpr int kSfbTiles = (BN + 127) / 128;   // a tile of 192 columns begins at the middle or at the beginning of one
   static constexpr int kSfBytes = (1 + kSfbTiles) * 512;
   static constexpr int kBlockBytes = kABytes + kBBytes;
   static constexpr int kStageBytes = kSub * kBlockBytes;
@@ -310,6 +310,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
           if (first) { follow(); first = false; }
           ok = mbar_wait_issuer(tempty_bar(acc), acc_ph ^ 1u, abort_flag, 0x42);
           if (!ok) break;
+          const uint32_t sfb_off = BN % 128 ? (uint32_t)(t.n0 & 127) / 32 : 0u;   // first scale column of the tile
           const int part = part_blocks<LONG>(t.blocks, C::kSub);
           int begin = 0;                            // of the part
           for (int kb = 0; kb < t.blocks; kb += C::kSub) {
@@ -332,7 +333,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
               if (!ok) break;
               tc_fence_after();
               const uint32_t idesc = instr_desc_mxf8(256, BN, 0) | byte << 4 | byte << 29;
-              const uint32_t sfa_t = tmem_base + C::kSfCol + q * 16, sfb_t = sfa_t + 4;
+              const uint32_t sfa_t = tmem_base + C::kSfCol + q * 16, sfb_t = sfa_t + 4 + sfb_off;
               const uint64_t adesc = operand_desc(st + u * C::kBlockBytes), bdesc = operand_desc(st + u * C::kBlockBytes + C::kABytes);
               const int n = GROUPS == 2 ? 4 : min(4, p.k_mmas - (kb + u) * 4);
               const bool last_of_slot = byte == 3u || kb + u == t.blocks - 1;
@@ -591,6 +592,22 @@ int launch(const Fp8Product& c, cudaStream_t s) {
   return fp8_blocks(c.K) > kMostBlocks ? launch<BN, GROUPS, true>(c, s) : launch<BN, GROUPS, false>(c, s);
 }
 
+template <int GROUPS>
+int launch_width(int width, const Fp8Product& c, cudaStream_t s) {
+  return width == 128 ? launch<128, GROUPS>(c, s) : width == 192 ? launch<192, GROUPS>(c, s) : launch<256, GROUPS>(c, s);
+}
+
+// Columns of a tile: the width whose waves of pairs take the least, a tile of 192 columns taking 0.86 and one of 128 0.68 of one of 256
+// (which alone has no second accumulator).  us, 256 / 192 columns: 2077 x 2840 x 1064 14.0 / 12.6, 1300 x 2000 x 2000 16.3 / 12.7, 8192 x 704
+// x 1064 18.6 / 14.6; with more waves 4096 x 2816 x 1024 15.7 / 16.3, 16384 x 4096 x 4096 193 / 221.  256 / 128: 1024 x 1024 x 1024 7.2 / 5.4,
+// 512 x 4096 x 11008 30.8 / 24.5; with two waves instead of one 2077 x 1064 x 2840 12.7 / 14.0.
+int tile_width(int64_t tiles_m, int64_t N) {
+  const int64_t pairs = sm_count() / 2;
+  auto cost = [&](int64_t width, int64_t per_tile) { return ceil_div(tiles_m * ceil_div(N, width), pairs) * per_tile; };
+  const int64_t wide = cost(256, 100), middle = cost(192, 86), narrow = cost(128, 68);
+  return wide <= middle && wide <= narrow ? 256 : middle <= narrow ? 192 : 128;
+}
+
 }  // namespace
 
 // Rows of A (of a segment, on average) up to which the product goes to gemm_fp8_few.cu: those that it takes at one time.  us, there / here:
@@ -602,11 +619,14 @@ int gemm_fp8(const Fp8Product& p, cudaStream_t s) {
   if (!p.experts && p.M <= kFewRows) return gemm_fp8_few(p, s);
   if (p.by_rows && p.counts && p.slots <= kFewRows * p.experts) return gemm_fp8_few(p, s);
   const int groups = p.experts == 0 ? 0 : p.by_rows ? 1 : 2;
-  const bool narrow = groups == 2 ? p.N <= 128 : pair_tile_width(p.M, p.N) == 128;
+  // rows of tiles; a segment's last tile is half empty on average
+  const int64_t tiles_m = groups == 0 ? ceil_div(p.M, 256) : groups == 2 ? p.experts * ceil_div(p.M, 256)
+                                                                      : ceil_div(p.slots ? std::min(p.slots, p.M) : p.M, 256) + p.experts / 2;
+  const int width = tile_width(tiles_m, p.N);
   switch (groups) {
-    case 0: return narrow ? launch<128, 0>(p, s) : launch<256, 0>(p, s);
-    case 1: return narrow ? launch<128, 1>(p, s) : launch<256, 1>(p, s);
-    default: return narrow ? launch<128, 2>(p, s) : launch<256, 2>(p, s);
+    case 0: return launch_width<0>(width, p, s);
+    case 1: return launch_width<1>(width, p, s);
+    default: return launch_width<2>(width, p, s);
   }
 }
 
