@@ -3,7 +3,8 @@
 // passing them through ctypes took 2.7 us of its 6 (three calls on kept weights: 18.4 -> 14.2 us, a 256-token step's two 29.1 -> 22.9).
 //
 // Argument rules, by what the C parameter is:
-//   pointer       a tensor or another object with data_ptr(), or None
+//   pointer       a tensor or another object with data_ptr(), or None; the FP8 and expert calls take tensors of the current device
+//                 only (the kernels run there, on its current stream), the others take their caller's word for it
 //   rounding      a Rounding (the class that bind() was given), or None
 //   dtype         an int, or a tensor (its dtype as an nvfp4_dtype): the parameters that NVFP4_CALLS lists
 //   size_t        an int, or a tensor (its number of elements): the size of the buffer before it
@@ -16,6 +17,7 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <dlfcn.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -49,10 +51,18 @@ const nvfp4_rounding* convert_rounding(PyObject* o) {
   return static_cast<const nvfp4_rounding*>(p);
 }
 
-template <typename T>
+// HERE: a tensor has to be on the current device.
+template <bool HERE, typename T>
 T convert_pointer(PyObject* o) {
   if (o == Py_None) return nullptr;
-  if (THPVariable_Check(o)) return static_cast<T>(THPVariable_Unpack(o).data_ptr());
+  if (THPVariable_Check(o)) {
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (HERE && !(t.is_cuda() && t.device().index() == c10::cuda::current_device())) {
+      PyErr_Format(PyExc_ValueError, "expected a tensor on the current CUDA device, got one on %s", t.device().str().c_str());
+      throw PythonError{};
+    }
+    return static_cast<T>(t.data_ptr());
+  }
   if (!PyObject_HasAttrString(o, "data_ptr")) type_error("a tensor or None", o);
   PyObject* const address = PyObject_CallMethod(o, "data_ptr", nullptr);   // a storage, say
   if (!address) throw PythonError{};
@@ -105,13 +115,13 @@ template <size_t... S>
 constexpr bool one_of(size_t i) { return ((i == S) || ...); }
 
 // DTYPES: the positions of the dtype parameters.
-template <size_t... DTYPES, typename... A, size_t... I>
+template <bool HERE, size_t... DTYPES, typename... A, size_t... I>
 PyObject* call(int (*f)(A...), PyObject* const* args, std::index_sequence<I...>) {
   constexpr size_t kLast = sizeof...(A) - 1;
   std::tuple<A...> a{[&]() -> A {
     if constexpr (I == kLast) return stream_handle(args[I]);
     else if constexpr (std::is_same_v<A, const nvfp4_rounding*>) return convert_rounding(args[I]);
-    else if constexpr (std::is_pointer_v<A>) return convert_pointer<A>(args[I]);
+    else if constexpr (std::is_pointer_v<A>) return convert_pointer<HERE, A>(args[I]);
     else return convert_number<A, one_of<DTYPES...>(I)>(args[I]);
   }()...};
   int st;
@@ -121,7 +131,7 @@ PyObject* call(int (*f)(A...), PyObject* const* args, std::index_sequence<I...>)
   return PyLong_FromLong(st);
 }
 
-template <size_t... DTYPES, typename... A>
+template <bool HERE, size_t... DTYPES, typename... A>
 PyObject* checked_call(int (*f)(A...), PyObject* const* args, Py_ssize_t n) {
   if (!f) {
     PyErr_SetString(PyExc_RuntimeError, "bind() first");
@@ -132,7 +142,7 @@ PyObject* checked_call(int (*f)(A...), PyObject* const* args, Py_ssize_t n) {
     return nullptr;
   }
   try {
-    return call<DTYPES...>(f, args, std::index_sequence_for<A...>{});
+    return call<HERE, DTYPES...>(f, args, std::index_sequence_for<A...>{});
   } catch (const PythonError&) {
     return nullptr;
   } catch (const std::exception& e) {              // torch's own checks (a tensor without storage, no GPU)
@@ -147,7 +157,8 @@ PyObject* checked_call(int (*f)(A...), PyObject* const* args, Py_ssize_t n) {
   X(nvfp4_gemm_quantized) X(nvfp4_gemm_mx, 10) X(nvfp4_gemm_bf16, 6) X(nvfp4_gemm_bf16_ex, 8) X(nvfp4_linear_fwd, 2, 12)    \
   X(nvfp4_linear_bwd_dx, 2, 12) X(nvfp4_linear_bwd_dw, 2, 12) X(nvfp4_linear_fwd_qout, 2) X(nvfp4_linear_fwd_qin, 4, 12)    \
   X(nvfp4_linear_fwd_save, 2, 14) X(nvfp4_linear_bwd_saved, 1, 12, 14) X(nvfp4_linear_bwd, 3, 16, 18)                       \
-  X(nvfp4_linear_bwd_bf16, 7, 9) X(nvfp4_linear_fwd_static, 2, 12)                                                          \
+  X(nvfp4_linear_bwd_bf16, 7, 9) X(nvfp4_linear_fwd_static, 2, 12)
+#define NVFP4_CALLS_HERE(X)                                                                                                 \
   X(nvfp4_quantize_fp8, 1) X(nvfp4_gemm_fp8, 8) X(nvfp4_linear_fp8_fwd, 2, 7) X(nvfp4_linear_fp8_bwd, 3, 8, 10)             \
   X(nvfp4_expert_sort) X(nvfp4_expert_gather, 1, 11) X(nvfp4_expert_combine, 1, 8) X(nvfp4_expert_combine_bwd, 1, 12)       \
   X(nvfp4_quantize_fp8_experts, 1, 11) X(nvfp4_gemm_fp8_experts, 12) X(nvfp4_gemm_fp8_experts_dw, 11)                       \
@@ -155,8 +166,17 @@ PyObject* checked_call(int (*f)(A...), PyObject* const* args, Py_ssize_t n) {
 
 #define NVFP4_WRAPPER(name, ...)                                                       \
   decltype(&::name) fn_##name = nullptr;                                               \
-  PyObject* py_##name(PyObject*, PyObject* const* args, Py_ssize_t n) { return checked_call<__VA_ARGS__>(fn_##name, args, n); }
+  PyObject* py_##name(PyObject*, PyObject* const* args, Py_ssize_t n) { return checked_call<kHere __VA_OPT__(,) __VA_ARGS__>(fn_##name, args, n); }
+namespace any_device {
+constexpr bool kHere = false;
 NVFP4_CALLS(NVFP4_WRAPPER)
+}  // namespace any_device
+namespace this_device {
+constexpr bool kHere = true;
+NVFP4_CALLS_HERE(NVFP4_WRAPPER)
+}  // namespace this_device
+using namespace any_device;
+using namespace this_device;
 
 // ---- outputs on the device of a given tensor ----
 PyObject* wrap(const at::Tensor& t) {
@@ -261,7 +281,7 @@ PyObject* py_bind(PyObject*, PyObject* args) {
   }
   bool all = true;
 #define NVFP4_BIND(name, ...) all = (fn_##name = reinterpret_cast<decltype(&::name)>(dlsym(lib, #name))) && all;
-  NVFP4_CALLS(NVFP4_BIND)
+  NVFP4_CALLS(NVFP4_BIND) NVFP4_CALLS_HERE(NVFP4_BIND)
   if (!all) {
     PyErr_Format(PyExc_OSError, "%s lacks entry points", file);
     return nullptr;
@@ -272,7 +292,7 @@ PyObject* py_bind(PyObject*, PyObject* args) {
 #define NVFP4_METHOD(name, ...) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr},
 #define NVFP4_HELPER(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"bind", py_bind, METH_VARARGS, nullptr}, NVFP4_HELPER(empty_fp8), NVFP4_HELPER(expert_buffers), NVFP4_HELPER(empty_rows),
-                         NVFP4_CALLS(NVFP4_METHOD){nullptr, nullptr, 0, nullptr}};
+                         NVFP4_CALLS(NVFP4_METHOD) NVFP4_CALLS_HERE(NVFP4_METHOD){nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -3,6 +3,10 @@
   python -m paper_2505_19115_b200.microbench gemm --m 8192 --n 8192 --k 4096 [--tile-n 256] [--bf16-out]
   python -m paper_2505_19115_b200.microbench quantize --rows 16384 --cols 16384 [--transposed] [--sr] [--fp32]
   python -m paper_2505_19115_b200.microbench amax --rows 16384 --cols 16384
+  python -m paper_2505_19115_b200.microbench gemm_fp8 --m 8192 --n 8192 --k 4096 [--bf16-out]
+  python -m paper_2505_19115_b200.microbench quantize_fp8 --rows 16384 --cols 16384 [--block-rows 128] [--transposed] [--fp32]
+  python -m paper_2505_19115_b200.microbench experts --tokens 16384 --topk 2 --experts 8 --k 1024 --n 2816
+      one training step of a layer of experts in FP8: sort, forward, combination, gradients, and each part by itself
 
   python -m paper_2505_19115_b200.microbench mma_peak [--stages 2048]
       the tensor pipe's issue rate for the GEMM's instruction, no loads: FLOP/clk/SM and TFLOP/s at the clock held
@@ -118,9 +122,37 @@ def gemm_account(m, n, k, bf16_out=False):
                               "accumulator_read_cycles_per_tile": a[13] / tiles_pair0}}
 
 
+def experts(a, dev):
+    """One training step of a layer of experts (tokens x k -> experts x n), and its parts."""
+    x, dy = synth.normal((a.tokens, a.k), 1.0, 1, device=dev), synth.normal((a.tokens, a.n), 1e-3, 2, device=dev)
+    W = synth.normal((a.experts, a.n, a.k), 0.02, 3, device=dev)
+    scores = torch.randn((a.tokens, a.experts), generator=torch.Generator(dev).manual_seed(4), device=dev)
+    value, expert_of = scores.topk(a.topk, 1)
+    w, expert_of = torch.softmax(value, 1).to(torch.bfloat16), expert_of.to(torch.int32)
+    plan = nb.nvfp4_expert_sort(expert_of, a.experts)
+    ws = torch.empty(max(nb.nvfp4_experts_fp8_workspace_bytes(a.tokens, a.topk, a.experts, a.n, a.k, k) for k in (nb.FP8_FWD, nb.FP8_BWD)),
+                     dtype=torch.uint8, device=dev)
+    Y = nb.nvfp4_experts_fp8_fwd(x, W, plan, workspace=ws)
+    dX, dW = nb.nvfp4_experts_fp8_bwd(dy, W, x, plan, weights=w, workspace=ws)
+    parts = {"sort": lambda: nb.nvfp4_expert_sort(expert_of, a.experts, plan),
+             "forward": lambda: nb.nvfp4_experts_fp8_fwd(x, W, plan, out=Y, workspace=ws),
+             "combine": lambda: nb.nvfp4_expert_combine(Y, plan, w),
+             "weights_gradient": lambda: nb.nvfp4_expert_combine_bwd(dy, Y, plan, w, rows_gradient=False),
+             "backward": lambda: nb.nvfp4_experts_fp8_bwd(dy, W, x, plan, weights=w, dX=dX, dW=dW, workspace=ws),
+             "input_gradient": lambda: nb.nvfp4_expert_combine(dX, plan)}
+    ms = _time(lambda: [f() for f in parts.values()], a.iters, a.warmup)
+    return {"kernel": "experts", "tokens": a.tokens, "topk": a.topk, "experts": a.experts, "n": a.n, "k": a.k, "rows": plan.rows, "ms": ms,
+            "TFLOP/s": 6.0 * a.tokens * a.topk * a.n * a.k / ms / 1e9, "parts_ms": {n: _time(f, a.iters, a.warmup) for n, f in parts.items()}}
+
+
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("kernel", choices=["gemm", "gemm_bf16", "transpose", "quantize", "dual", "amax", "mma_peak", "gemm_account"])
+    ap.add_argument("kernel", choices=["gemm", "gemm_bf16", "gemm_fp8", "transpose", "quantize", "quantize_fp8", "dual", "amax", "experts",
+                                       "mma_peak", "gemm_account"])
+    ap.add_argument("--tokens", type=int, default=16384)
+    ap.add_argument("--topk", type=int, default=2)
+    ap.add_argument("--experts", type=int, default=8)
+    ap.add_argument("--block-rows", type=int, default=1)
     ap.add_argument("--stages", type=int, default=2048)
     ap.add_argument("--instr-n", type=int, default=256)
     ap.add_argument("--m", type=int, default=8192)
@@ -164,6 +196,20 @@ def main():
         ms = _time(lambda: nb.nvfp4_gemm_bf16(A, B, out=out), a.iters, a.warmup)
         res = {"kernel": "gemm_bf16", "m": a.m, "n": a.n, "k": a.k, "out": str(out.dtype), "ms": ms,
                "TFLOP/s": 2.0 * a.m * a.n * a.k / ms / 1e9}
+    elif a.kernel == "gemm_fp8":
+        ac, asf, _, _ = nb.nvfp4_quantize_fp8(synth.normal((a.m, a.k), 1.0, 1, device=dev))
+        bc, bsf, _, _ = nb.nvfp4_quantize_fp8(synth.normal((a.n, a.k), 0.02, 2, device=dev), 128)
+        out = torch.empty((a.m, a.n), dtype=torch.bfloat16 if a.bf16_out else torch.float32, device=dev)
+        ms = _time(lambda: nb.nvfp4_gemm_fp8(ac, asf, bc, bsf, out=out), a.iters, a.warmup)
+        res = {"kernel": "gemm_fp8", "m": a.m, "n": a.n, "k": a.k, "out": str(out.dtype), "ms": ms, "TFLOP/s": 2.0 * a.m * a.n * a.k / ms / 1e9,
+               "GB/s": (a.m * a.k + a.n * a.k + a.m * a.n * out.element_size()) / ms / 1e6}
+    elif a.kernel == "quantize_fp8":
+        x = synth.heavy_tailed((a.rows, a.cols), 1002, device=dev, dtype=torch.float32 if a.fp32 else torch.bfloat16)
+        ms = _time(lambda: nb.nvfp4_quantize_fp8(x, a.block_rows, True, a.transposed), a.iters, a.warmup)
+        res = {"kernel": "quantize_fp8", "rows": a.rows, "cols": a.cols, "block_rows": a.block_rows, "both": a.transposed, "dtype": str(x.dtype),
+               "ms": ms, "GB/s": a.rows * a.cols * (x.element_size() + 1 + a.transposed) / ms / 1e6}
+    elif a.kernel == "experts":
+        res = experts(a, dev)
     elif a.kernel == "transpose":
         x = synth.normal((a.rows, a.cols), 1.0, 3, device=dev)
         ms = _time(lambda: nb.nvfp4_transpose_bf16(x), a.iters, a.warmup)

@@ -126,3 +126,37 @@ def test_expert_choices_are_whole_numbers():
         is_cuda = True
     with pytest.raises(TypeError):
         nb.nvfp4_expert_sort(torch.zeros((2, 2)).as_subclass(OnDevice), 4)
+
+
+HERE = ("nvfp4_quantize_fp8", "nvfp4_gemm_fp8", "nvfp4_linear_fp8_fwd", "nvfp4_linear_fp8_bwd", "nvfp4_expert_sort", "nvfp4_expert_gather", "nvfp4_expert_combine",
+        "nvfp4_expert_combine_bwd", "nvfp4_quantize_fp8_experts", "nvfp4_gemm_fp8_experts", "nvfp4_gemm_fp8_experts_dw", "nvfp4_experts_fp8_fwd", "nvfp4_experts_fp8_bwd")
+
+
+@pytest.mark.parametrize("name", HERE)
+def test_tensors_elsewhere_are_refused(name):
+    # a kernel would read a host tensor's address, or another device's memory, on the current device
+    argtypes = getattr(nb.lib(), name).argtypes
+    class Stream:
+        cuda_stream = 0
+    args = [None if t is C.c_void_p else 0 for t in argtypes[:-1]] + [Stream]
+    for i, t in enumerate(argtypes[:-1]):
+        if t is C.c_void_p:
+            with pytest.raises((ValueError, RuntimeError)):       # RuntimeError: no CUDA device to be current
+                getattr(nb._native(), name)(*args[:i], torch.zeros(64), *args[i + 1:])
+
+
+def test_outputs_are_laid_out_as_the_calls_take_them():
+    n, like = nb._native(), torch.zeros(1)
+    codes, sf, codes_t, sf_t = n.empty_fp8(like, 0, 130, 24, 1, 1, nb.SF_SWIZZLED)
+    assert codes.shape == (130, 24) and codes.stride() == (32, 1) and codes_t.shape == (24, 130) and codes_t.stride() == (144, 1)
+    assert codes.untyped_storage().nbytes() == nb.nvfp4_codes_bytes_fp8(130, 24) and sf.numel() == nb.nvfp4_sf_bytes_fp8(130, 24)
+    assert codes_t.untyped_storage().nbytes() == nb.nvfp4_codes_bytes_fp8(24, 130) and sf_t.numel() == nb.nvfp4_sf_bytes_fp8(24, 130)
+    codes, sf, none, none_t = n.empty_fp8(like, 3, 130, 264, 1, 0, nb.SF_LINEAR)
+    assert codes.shape == (3, 130, 264) and codes.stride() == (130 * 272, 272, 1) and sf.shape == (3, 130, 3) and none is none_t is None
+    assert [t.shape for t in n.expert_buffers(like, 5, 2, 3, 256)] == [(3,), (4,), (5, 2), (256,)]
+    assert n.empty_rows(like.to(torch.bfloat16), 4, 8).dtype == torch.bfloat16
+    for bad in (lambda: n.empty_fp8(like, 0, 1, 1, 1, 0), lambda: n.empty_fp8(5, 0, 1, 1, 1, 0, 1), lambda: n.empty_rows(like, 1.5, 8), lambda: n.expert_buffers(like, 1, 1, 1, None)):
+        with pytest.raises(TypeError):
+            bad()
+    with pytest.raises(RuntimeError):
+        n.empty_rows(like, -1, 8)
