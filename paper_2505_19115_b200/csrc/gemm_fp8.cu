@@ -35,10 +35,10 @@ constexpr int kControlRegs = 72, kEpilogueRegs = 184;   // 256 x (72 + 184) = 65
 template <int BN>
 struct Cfg {
   // Blocks per k-stage.  The roles' hand-over of a stage takes about as long as a block's instructions of 128 columns, so that narrow
-  // tiles take two blocks at a time (us, one / two: 704 x 704 x 16384 35.0 / 30.3, 512 x 4096 x 11008 27.4 / 24.5); wide ones lose by it
-  // what the ring has in depth (16384 x 1024 x 2816 41.1 / 41.8).
-  static constexpr int kSub = BN == 128 ? 2 : 1;
-  static constexpr int kStages = BN == 128 ? 4 : 6;
+  // tiles take two blocks at a time (us, one / two: 704 x 704 x 16384 35.0 / 30.3, 512 x 4096 x 11008 27.4 / 24.5; 192 columns 16384 x
+  // 4096 x 4096 213 / 200); wide ones lose by it what the ring has in depth (16384 x 1024 x 2816 41.1 / 41.8).
+  static constexpr int kSub = BN == 256 ? 1 : 2;
+  static constexpr int kStages = BN == 128 ? 4 : BN == 192 ? 3 : 6;
   static constexpr int kAccStages = BN == 256 ? 1 : 2;
   static constexpr int kABytes = 128 * kBK;
   static constexpr int kBBytes = (BN / 2) * kBK;
@@ -597,14 +597,14 @@ int launch_width(int width, const Fp8Product& c, cudaStream_t s) {
   return width == 128 ? launch<128, GROUPS>(c, s) : width == 192 ? launch<192, GROUPS>(c, s) : launch<256, GROUPS>(c, s);
 }
 
-// Columns of a tile: the width whose waves of pairs take the least, a tile of 192 columns taking 0.86 and one of 128 0.68 of one of 256
-// (which alone has no second accumulator).  us, 256 / 192 columns: 2077 x 2840 x 1064 14.0 / 12.6, 1300 x 2000 x 2000 16.3 / 12.7, 8192 x 704
-// x 1064 18.6 / 14.6; with more waves 4096 x 2816 x 1024 15.7 / 16.3, 16384 x 4096 x 4096 193 / 221.  256 / 128: 1024 x 1024 x 1024 7.2 / 5.4,
+// Columns of a tile: the width whose waves of pairs take the least, a tile of 192 columns taking 0.83 and one of 128 0.68 of one of 256
+// (which alone has no second accumulator).  us, 256 / 192 columns: 2077 x 2840 x 1064 14.3 / 13.0, 2077 x 1064 x 2840 12.8 / 11.1, 8192 x 1064
+// x 712 16.4 / 14.7; with more waves 4096 x 2816 x 1024 16.2 / 16.9, 16384 x 4096 x 4096 197 / 219.  256 / 128: 1024 x 1024 x 1024 7.2 / 5.4,
 // 512 x 4096 x 11008 30.8 / 24.5; with two waves instead of one 2077 x 1064 x 2840 12.7 / 14.0.
 int tile_width(int64_t tiles_m, int64_t N) {
   const int64_t pairs = sm_count() / 2;
   auto cost = [&](int64_t width, int64_t per_tile) { return ceil_div(tiles_m * ceil_div(N, width), pairs) * per_tile; };
-  const int64_t wide = cost(256, 100), middle = cost(192, 86), narrow = cost(128, 68);
+  const int64_t wide = cost(256, 100), middle = cost(192, 83), narrow = cost(128, 68);
   return wide <= middle && wide <= narrow ? 256 : middle <= narrow ? 192 : 128;
 }
 

@@ -8,7 +8,8 @@
 // time.  us, weights that are in no cache (floor: their bytes at the rate of a copy): 11008 x 4096 (7.0) 1 row 12.0, 67 rows 13.0, 128 rows
 // 13.7; 4096 x 11008 (7.0) 11.6, 13.3, 14.9; 4096 x 4096 (2.6) 6.8, 8.9, 10.3.  With gemm_fp8.cu's kernel 15-16, 23, 11; with dot products by
 // mma.sync, 16 rows of B a block, 11.0, 15.2 and 7.3 for up to 8 rows, and twice that for 16.  About 3 us are a launch and the first and
-// last latencies; an instruction of 128 rows takes about 115 cycles however few its columns, 2 us in all of the 12.
+// last latencies; an instruction of 128 rows takes about 115 cycles however few its columns, but pairs of CTAs, whose instructions of
+// 256 rows take 40 to 64, gain nothing in all (11.8) and lose where clusters of eight blocks do not all find room (4096 x 11008 19.8).
 //
 // One product: with few tiles of B a cluster of 2, 4 or 8 blocks shares one along the contraction axis; each then sums a share of
 // the tokens over all blocks' accumulators, which they write into one another's shared memory, in the order of the blocks.
