@@ -144,7 +144,7 @@ extern "C" int nvfp4_experts_fp8_fwd(const void* X, int x_by_token, const void* 
   const Fp8Operand ops[2] = {{W, experts, N, K, K, 1, ws + l.w.codes, ws + l.w.sf, nullptr, nullptr, {}},
                              {X, 1, R, K, K, 0, ws + l.x.codes, ws + l.x.sf, nullptr, nullptr, from}};
   if (int st = quantize_fp8(ops, 2, dtype, NVFP4_SF_SWIZZLED_128x4, s)) return st;
-  return gemm_fp8({ws + l.x.codes, ws + l.x.sf, ws + l.w.codes, ws + l.w.sf, R, N, K, Y, y_dtype, N, experts, offsets, true}, s);
+  return gemm_fp8({ws + l.x.codes, ws + l.x.sf, ws + l.w.codes, ws + l.w.sf, R, N, K, Y, y_dtype, N, experts, offsets, true, nullptr, tokens * topk}, s);
 }
 
 extern "C" int nvfp4_experts_fp8_bwd(const void* dY, int dy_by_token, const void* dy_weights, int weights_dtype, const void* W, const void* X,
@@ -171,7 +171,9 @@ extern "C" int nvfp4_experts_fp8_bwd(const void* dY, int dy_by_token, const void
                              {X, 1, R, K, K, 0, nullptr, nullptr, ws + l.xt.codes, ws + l.xt.sf, x_from},
                              {dY, 1, R, N, N, 0, ws + l.dy.codes, ws + l.dy.sf, ws + l.dyt.codes, ws + l.dyt.sf, dy_from}};
   if (int st = quantize_fp8(ops, 3, dtype, NVFP4_SF_SWIZZLED_128x4, s)) return st;
-  if (int st = gemm_fp8({ws + l.dy.codes, ws + l.dy.sf, ws + l.wt.codes, ws + l.wt.sf, R, K, N, dX, dx_dtype, K, experts, offsets, true}, s)) return st;
+  if (int st = gemm_fp8({ws + l.dy.codes, ws + l.dy.sf, ws + l.wt.codes, ws + l.wt.sf, R, K, N, dX, dx_dtype, K, experts, offsets, true, nullptr,
+                         tokens * topk}, s))
+    return st;
   Fp8Product dw = {ws + l.dyt.codes, ws + l.dyt.sf, ws + l.xt.codes, ws + l.xt.sf, N, K, R, dW, dw_dtype, K, experts, offsets, false};
   dw.late = true;
   return gemm_fp8(dw, s);

@@ -8,9 +8,10 @@
 // thread's own rows and then, through shared memory, over the warps.  Row codes leave from registers, 128 bytes of a row per
 // half warp; transposed ones are packed along the thread's 8 rows and turned round in shared memory.  Nothing behind the last row or
 // column is written.
-// 8192 x 8192 bf16 (buffers in turn, nothing in the caches): row output 31 us = 6.5 TB/s, transposed 35 = 5.7, both 48 = 5.6; 16384 x
-// 11008 78 / 89 / 123 us = 6.9 / 6.1 / 5.9; fp32 8192 x 8192 50 / 53 / 70.  (A copy: 6.3-6.5 TB/s.)  With a branch around each load,
+// 8192 x 8192 bf16 (buffers in turn, nothing in the caches): row output 32 us = 6.3 TB/s, transposed 32.6 = 6.2, both 47 = 5.7; 16384 x
+// 11008 79 / 82 / 120 us = 6.8 / 6.6 / 6.0; fp32 8192 x 8192 52 / 54 / 72.  (A copy: 6.3-6.5 TB/s.)  With a branch around each load,
 // 64-bit tile indices and a shuffled maximum per row the kernel was bound by instruction issue (18.6 per element): both 74 us.
+// 33000 rows of 2816 gathered from 16384, both outputs: 70 us, with weights 92.
 #include <cuda_bf16.h>
 
 #include <type_traits>
@@ -176,7 +177,7 @@ __device__ __forceinline__ void store_codes(uint8_t* dst, int n, uint32_t lo, ui
 }
 
 // The maxima of a thread's 8 rows -> the one of row l16 / 2 over all 16 lanes.  Each step hands half of the rows to the other lane
-// of a pair, so that 8 + 1 exchanges (5 on packed halves) do what 32 would, and a row's scale is computed by one lane pair, not by all.
+// of a pair, so that 8 exchanges do what 32 would, and a row's scale is computed by one lane pair, not by all.
 __device__ __forceinline__ uint32_t own_row_max(const uint32_t (&m)[8], int l16) {
   uint32_t a[4], b[2], c;
 #pragma unroll
@@ -221,8 +222,8 @@ __global__ void __launch_bounds__(256, std::is_same_v<T, __nv_bfloat16> ? WEIGHT
   const T* const x = static_cast<const T*>(o.x) + b * o.rows * o.ld + col;
   const int left = (int)min((int64_t)8, o.cols - col);
   // Loads wait for no branch: rows that do not exist are loaded from one that does (columns likewise) and cleared afterwards.  Only
-  // a row's last few values, where their number is no multiple of 8, are fetched one by one.
-  const bool some = left > 0 && left < 8;
+  // a row's last few values, where their number is no multiple of 8, are fetched one by one, and rows of fewer than 8 as a whole.
+  const bool some = left > 0 && left < 8, eight = o.cols >= 8;
   const T* const from = left < 8 ? x - col : x;
   if (o.from.slot_of) {                                  // rows: a multiple of 128
     // lane i of a half warp finds row i's source
@@ -234,7 +235,8 @@ __global__ void __launch_bounds__(256, std::is_same_v<T, __nv_bfloat16> ? WEIGHT
       if (o.from.weights && slot >= 0) weight = load_weight(o.from.weights, o.from.weights_dtype, slot);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      v.load(i, from + (int64_t)max(__shfl_sync(0xFFFFFFFFu, source, i, 16), 0) * o.ld);
+      const int r = max(__shfl_sync(0xFFFFFFFFu, source, i, 16), 0);
+      if (eight) v.load(i, from + (int64_t)r * o.ld);
     }
     if (c0 + 128 > o.cols || __any_sync(0xFFFFFFFFu, source < 0)) {
 #pragma unroll
@@ -254,7 +256,8 @@ __global__ void __launch_bounds__(256, std::is_same_v<T, __nv_bfloat16> ? WEIGHT
     for (int i = 0; i < 8; ++i) v.load(i, src + i * o.ld);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v.load(i, from + min(row + i, o.rows - 1) * o.ld);
+    for (int i = 0; i < 8; ++i)
+      if (eight) v.load(i, from + min(row + i, o.rows - 1) * o.ld);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if (row + i >= o.rows || left < 8) v.clear(i);

@@ -173,7 +173,10 @@ __global__ void __launch_bounds__(kSortThreads, 1) expert_sort_kernel(const Sort
 
 // ------------------------------------------------------------------------------------------------
 // Moving rows.  All three are bound by memory, in units of 16 bytes of a row.  What they read first are indices, so a warp fetches
-// all that it needs at once (a lane each) and then has 4 to 8 units per lane in flight.
+// all that it needs at once (a lane each) and then has 4 to 12 units per lane in flight; it works in the order of tokens, so that a
+// token's row is read once however many choices it has.
+// 16384 tokens, two of 8 experts, bf16 (buffers in turn): 4096 columns gather 70 us = 5.8 TB/s (two thirds of it written), combine 61 =
+// 6.6, its gradient 107 = 6.3, that of the weights alone 60 = 6.7; 2816 columns 50 / 45 / 76 / 43.  The sort 7 us (one token 3.7).
 // ------------------------------------------------------------------------------------------------
 template <typename T>
 constexpr int kUnit = 16 / (int)sizeof(T);           // values per unit
@@ -462,7 +465,7 @@ bool dtype_ok(int dtype) { return dtype == NVFP4_BF16 || dtype == NVFP4_FP32; }
 using namespace nvfp4;
 
 extern "C" int64_t nvfp4_expert_rows(int64_t tokens, int64_t topk, int64_t experts) {
-  constexpr int64_t kMost = (1ll << 31) - 512;
+  constexpr int64_t kMost = (1ll << 31) - 65536;    // an index of a row or a slot, and the strides of the loops over them
   if (tokens <= 0 || topk <= 0 || experts <= 0 || experts > kMaxExperts || topk > kMost / tokens) return 0;
   const int64_t n = tokens * topk, rows = (n + (kFp8Block - 1) * std::min(n, experts)) / kFp8Block * kFp8Block;
   return rows <= kMost ? rows : 0;

@@ -72,7 +72,8 @@ def _reference(plan):
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("w_dtype", [None, torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("size", [(1, 8, 16, 64), (5, 1, 3, 8), (300, 2, 8, 520), (129, 6, 40, 1032), (1000, 5, 7, 2048)])
+@pytest.mark.parametrize("size", [(1, 8, 16, 64), (5, 1, 3, 8), (300, 2, 8, 520), (129, 6, 40, 1032), (1000, 5, 7, 2048), (40, 40, 64, 72),
+                                  (3000, 3, 6, 264), (2500, 1, 4, 1032), (2400, 34, 40, 136)])
 def test_rows_moved_and_summed_with_gradients(size, w_dtype, dtype):
     T, topk, E, H = size
     plan = nb.nvfp4_expert_sort(_choices(T, topk, E, T, 0.2), E)
@@ -391,3 +392,49 @@ def test_weights_and_values_next_to_the_smallest_and_the_largest_numbers(dtype):
             assert torch.equal(c[keep], ref.code_bytes(y)[keep])
             assert torch.equal(got[~bad], ref.scale_bytes(e)[~bad])
             assert bool((c[~keep] & 127 == 127).all())
+
+
+def test_two_streams_at_once_with_workspaces_of_their_own():
+    T, topk, E, N, K = 700, 2, 6, 328, 392
+    work = [(_normal((T, K), 10 + i), _normal((T, N), 20 + i), _normal((E, N, K), 30 + i, std=0.05), _normal((T, topk), 40 + i, torch.float32),
+             _choices(T, topk, E, 50 + i), E, _workspace(T, topk, E, N, K)) for i in range(2)]
+    want = []
+    for w in work:
+        want.append(_step(*w))
+        torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in work]
+    got = [None, None]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(6):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i] = _step(*work[i])
+    torch.cuda.synchronize()
+    assert nb.nvfp4_device_error_word() == 0
+    for g, w in zip(got, want):
+        assert all(torch.equal(a, b) for a, b in zip(g, w))
+
+
+def test_few_rows_of_experts_in_every_number():
+    # the product of few rows for each expert: none, one, those of a tile and more than a tile, and experts that share nothing
+    E, N, K = 7, 392, 648
+    W = _normal((E, N, K), 1, std=0.05)
+    wc, ws, _, _ = nb.nvfp4_quantize_fp8(W, 128)
+    for counts in ([0, 1, 2, 15, 16, 17, 0], [128, 0, 0, 129, 31, 33, 1], [300, 0, 0, 0, 0, 0, 0], [0, 0, 0, 0, 0, 0, 1]):
+        expert_of = torch.repeat_interleave(torch.arange(E), torch.tensor(counts))[torch.randperm(sum(counts), generator=torch.Generator().manual_seed(1))]
+        expert_of = expert_of.int().cuda()[:, None].contiguous()
+        plan = nb.nvfp4_expert_sort(expert_of, E)
+        assert plan.counts.tolist() == counts
+        x = _normal((len(expert_of), K), 2)
+        xc, xs, _, _ = nb.nvfp4_quantize_fp8_experts(x, plan)
+        rows = nb.nvfp4_expert_gather(x, plan)
+        for dtype in (torch.float32, torch.bfloat16):
+            Y = torch.full((plan.rows, N), 5.0, dtype=dtype, device="cuda")
+            nb.nvfp4_gemm_fp8_experts(xc, xs, wc, ws, plan, out=Y)
+            torch.cuda.synchronize()
+            assert nb.nvfp4_device_error_word() == 0
+            assert bool((Y[int(plan.offsets[-1]):] == 5).all())
+            for e, begin, end in _segments(plan):
+                if begin < end:
+                    ref.assert_product(Y[begin:end], *ref.product(ref.values(rows[begin:end]), ref.values(W[e], True)), K)

@@ -38,7 +38,7 @@ def _check_quantized(x, block_rows, sf_layout, codes, scales, codes_t, scales_t)
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("block_rows", [1, 128])
 @pytest.mark.parametrize("sf_layout", [nb.SF_LINEAR, nb.SF_SWIZZLED])
-@pytest.mark.parametrize("shape", [(1, 1), (1, 8), (7, 130), (128, 128), (129, 136), (300, 1031), (513, 640), (16, 2056)])
+@pytest.mark.parametrize("shape", [(1, 1), (1, 8), (200, 3), (7, 130), (128, 128), (129, 136), (300, 1031), (513, 640), (16, 2056)])
 def test_quantizer_matches_the_definition(shape, sf_layout, block_rows, dtype):
     rows, cols = shape
     x = _x((rows, -(-cols // 8) * 8), rows + cols, dtype)[:, :cols]
