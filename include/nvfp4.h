@@ -417,8 +417,8 @@ NVFP4_API int nvfp4_expert_combine_bwd(const void* dy, int dtype, int64_t tokens
  * nvfp4_gemm_fp8_experts_dw: D[e] = A[:, segment e] . B[:, segment e]^T: A [N, R] and B [K, R], the transposed outputs of the
  *   rows' quantization, D [experts, N, K] dense.  An expert without rows gets zeros.
  * nvfp4_experts_fp8_fwd / _bwd: the layer: Y [R, N] from X; dX [R, K] and dW [experts, N, K] from dY, W and X.  x_by_token / dy_by_token and
- *   dy_weights as by_token and weights above (the weighted sum's output gradient goes in as it is).  Padding rows of Y and dX are zero.  N and K multiples of 8, everything
- *   dense and 16-byte aligned, workspace of nvfp4_experts_fp8_workspace_bytes(..., which) bytes as for nvfp4_linear_fp8_*.
+ *   dy_weights as by_token and weights above (the weighted sum's output gradient goes in as it is).  Padding rows of Y and dX are
+ *   zero.  N and K multiples of 8, everything dense and 16-byte aligned, workspace of nvfp4_experts_fp8_workspace_bytes(..., which) bytes as for nvfp4_linear_fp8_*.
  */
 NVFP4_API int nvfp4_quantize_fp8_experts(const void* x, int dtype, int by_token, int64_t tokens, int64_t topk, int64_t experts, int64_t cols,
                                int64_t ld, const int32_t* offsets, const int32_t* slot_of, const void* weights, int weights_dtype,

@@ -534,15 +534,11 @@ def nvfp4_sf_bytes_fp8(Rq: int, Kq: int, sf_layout: int = SF_SWIZZLED) -> int:
     return int(lib().nvfp4_sf_bytes_fp8(Rq, Kq, sf_layout))
 
 
-def _fp8_operand(codes):
-    """(matrices, Rq, Kq) of codes as the quantizer leaves them."""
-    shape, stride = codes.shape, codes.stride()
-    Rq, Kq = shape[-2:]
-    pitch = -(-Kq // 16) * 16
-    if codes.element_size() != 1 or stride[-1] != 1 or (Rq > 1 and stride[-2] != pitch) or (
-            len(shape) == 3 and shape[0] > 1 and stride[0] != Rq * pitch):
-        raise ValueError("FP8 codes have one byte each and rows of a multiple of 16 bytes, one behind the other")
-    return shape[0] if len(shape) == 3 else 1, Rq, Kq
+def _product_rows(M, N, dtype, device):
+    """[M, N] with rows of a multiple of 16 bytes."""
+    whole = 16 // dtype.itemsize
+    out = torch.empty((M, -(-N // whole) * whole), dtype=dtype, device=device)
+    return out if N % whole == 0 else out[:, :N]
 
 
 def nvfp4_quantize_fp8(x, block_rows: int = 1, row: bool = True, transposed: bool = False, sf_layout: int = SF_SWIZZLED, stream=None):
@@ -564,12 +560,13 @@ def nvfp4_quantize_fp8(x, block_rows: int = 1, row: bool = True, transposed: boo
 
 def nvfp4_gemm_fp8(a_codes, a_sf, b_codes, b_sf, out_dtype=torch.float32, out=None, stream=None):
     """D[M,N] = A[M,K] . B[N,K]^T on FP8 codes with swizzled scales."""
-    (_, M, K), (_, N, Kb) = _fp8_operand(a_codes), _fp8_operand(b_codes)
-    assert K == Kb
+    native = _native()
+    (a, M, K), (b, N, Kb) = native.fp8_operand(a_codes, a_sf), native.fp8_operand(b_codes, b_sf)
+    assert K == Kb and a == b == 1
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype, device=a_codes.device)
+        out = _product_rows(M, N, out_dtype, a_codes.device)
     assert out.shape == (M, N) and out.stride(1) == 1
-    st = _native().nvfp4_gemm_fp8(a_codes, a_sf, b_codes, b_sf, M, N, K, out, out, out.stride(0), stream)
+    st = native.nvfp4_gemm_fp8(a_codes, a_sf, b_codes, b_sf, M, N, K, out, out, out.stride(0), stream)
     _check(st, "nvfp4_gemm_fp8")
     return out
 
@@ -715,12 +712,13 @@ def nvfp4_quantize_fp8_experts(x, plan, weights=None, sorted_rows: bool = False,
 
 def nvfp4_gemm_fp8_experts(a_codes, a_sf, b_codes, b_sf, plan, out_dtype=torch.float32, out=None, stream=None):
     """D[r] = A[r] . B[e]^T for the rows r of expert e; A [rows, K], B [experts, N, K]."""
-    (_, R, K), (E, N, Kb) = _fp8_operand(a_codes), _fp8_operand(b_codes)
-    assert K == Kb and R == plan.rows and E == plan.experts
+    native = _native()
+    (a, R, K), (E, N, Kb) = native.fp8_operand(a_codes, a_sf), native.fp8_operand(b_codes, b_sf)
+    assert K == Kb and a == 1 and R == plan.rows and E == plan.experts
     if out is None:
-        out = torch.empty((R, N), dtype=out_dtype, device=a_codes.device)
+        out = _product_rows(R, N, out_dtype, a_codes.device)
     assert out.shape == (R, N) and out.stride(1) == 1
-    st = _native().nvfp4_gemm_fp8_experts(a_codes, a_sf, b_codes, b_sf, plan.tokens, plan.topk, E, plan.counts, plan.offsets, N, K, out, out,
+    st = native.nvfp4_gemm_fp8_experts(a_codes, a_sf, b_codes, b_sf, plan.tokens, plan.topk, E, plan.counts, plan.offsets, N, K, out, out,
                                           out.stride(0), stream)
     _check(st, "nvfp4_gemm_fp8_experts")
     return out
@@ -728,12 +726,13 @@ def nvfp4_gemm_fp8_experts(a_codes, a_sf, b_codes, b_sf, plan, out_dtype=torch.f
 
 def nvfp4_gemm_fp8_experts_dw(a_codes, a_sf, b_codes, b_sf, plan, out_dtype=torch.float32, out=None, stream=None):
     """D[e] = A[:, rows of e] . B[:, rows of e]^T; A [N, rows], B [K, rows] (transposed outputs of nvfp4_quantize_fp8_experts)."""
-    (_, N, R), (_, K, Rb) = _fp8_operand(a_codes), _fp8_operand(b_codes)
-    assert R == Rb == plan.rows
+    native = _native()
+    (a, N, R), (b, K, Rb) = native.fp8_operand(a_codes, a_sf), native.fp8_operand(b_codes, b_sf)
+    assert a == b == 1 and R == Rb == plan.rows
     if out is None:
         out = torch.empty((plan.experts, N, K), dtype=out_dtype, device=a_codes.device)
     assert out.shape == (plan.experts, N, K) and out.is_contiguous()
-    st = _native().nvfp4_gemm_fp8_experts_dw(a_codes, a_sf, b_codes, b_sf, plan.tokens, plan.topk, plan.experts, plan.offsets, N, K, out, out, stream)
+    st = native.nvfp4_gemm_fp8_experts_dw(a_codes, a_sf, b_codes, b_sf, plan.tokens, plan.topk, plan.experts, plan.offsets, N, K, out, out, stream)
     _check(st, "nvfp4_gemm_fp8_experts_dw")
     return out
 

@@ -265,6 +265,38 @@ PyObject* py_empty_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return nullptr;
 }
 
+// fp8_operand(codes, scales): (matrices, Rq, Kq) of codes as the quantizer leaves them, with swizzled scales.  Other layouts and buffers
+// that are too small are refused: the products would read behind them.
+PyObject* py_fp8_operand(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 2) {
+    PyErr_SetString(PyExc_TypeError, "expected 2 arguments");
+    return nullptr;
+  }
+  try {
+    const at::Tensor &codes = tensor(args[0]), &scales = tensor(args[1]);
+    const int64_t d = codes.dim();
+    if ((d != 2 && d != 3) || codes.element_size() != 1) {
+      PyErr_SetString(PyExc_ValueError, "FP8 codes have one byte each and two or three dimensions");
+      return nullptr;
+    }
+    const int64_t b = d == 3 ? codes.size(0) : 1, rq = codes.size(d - 2), kq = codes.size(d - 1), pitch = (kq + 15) / 16 * 16;
+    if (codes.stride(d - 1) != 1 || (rq > 1 && codes.stride(d - 2) != pitch) || (b > 1 && codes.stride(0) != rq * pitch)) {
+      PyErr_SetString(PyExc_ValueError, "rows of FP8 codes take a multiple of 16 bytes and lie one behind the other");
+      return nullptr;
+    }
+    const int64_t tiles = b * ((rq + 127) / 128) * (((kq + 127) / 128 + 3) / 4);
+    if (scales.element_size() != 1 || !scales.is_contiguous() || scales.numel() < tiles * 512) {
+      PyErr_SetString(PyExc_ValueError, "FP8 codes come with a flat buffer of swizzled scales");
+      return nullptr;
+    }
+    return Py_BuildValue("(LLL)", (long long)b, (long long)rq, (long long)kq);
+  } catch (const PythonError&) {
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+  }
+  return nullptr;
+}
+
 // bind(path, Rounding): takes the entry points from the library at `path`, and the class of the rounding descriptors.
 PyObject* py_bind(PyObject*, PyObject* args) {
   const char* file;
@@ -291,7 +323,7 @@ PyObject* py_bind(PyObject*, PyObject* args) {
 
 #define NVFP4_METHOD(name, ...) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr},
 #define NVFP4_HELPER(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {{"bind", py_bind, METH_VARARGS, nullptr}, NVFP4_HELPER(empty_fp8), NVFP4_HELPER(expert_buffers), NVFP4_HELPER(empty_rows),
+PyMethodDef methods[] = {{"bind", py_bind, METH_VARARGS, nullptr}, NVFP4_HELPER(empty_fp8), NVFP4_HELPER(expert_buffers), NVFP4_HELPER(empty_rows), NVFP4_HELPER(fp8_operand),
                          NVFP4_CALLS(NVFP4_METHOD) NVFP4_CALLS_HERE(NVFP4_METHOD){nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -121,6 +121,22 @@ def test_codes_that_are_not_laid_out_as_the_quantizer_leaves_them_are_refused():
             nb.nvfp4_gemm_fp8(bad, sf, good, sf, out=torch.zeros((4, 4)))
 
 
+def test_scales_of_another_layout_are_refused():
+    # the products would read behind them
+    good, sf = torch.zeros((200, 528), dtype=torch.uint8), torch.zeros(2 * 2 * 512, dtype=torch.uint8)
+    n = nb._native()
+    assert n.fp8_operand(good, sf) == (1, 200, 528)
+    assert n.fp8_operand(good[:, :520], sf) == (1, 200, 520)
+    assert n.fp8_operand(good.view(4, 50, 528), torch.zeros(4 * 2 * 512, dtype=torch.uint8)) == (4, 50, 528)
+    for bad in (torch.zeros((200, 5), dtype=torch.uint8), sf[:-1], torch.zeros(512, dtype=torch.int32), torch.zeros(4096, dtype=torch.uint8)[::2]):
+        for operands in ((good, bad, good, sf), (good, sf, good, bad)):
+            with pytest.raises(ValueError):
+                nb.nvfp4_gemm_fp8(*operands, out=torch.zeros((200, 200)))
+    for bad in ((good,), (good, None), (1, sf)):
+        with pytest.raises(TypeError):
+            n.fp8_operand(*bad)
+
+
 def test_expert_choices_are_whole_numbers():
     class OnDevice(torch.Tensor):
         is_cuda = True

@@ -287,3 +287,13 @@ def test_products_of_few_rows(M, out_dtype):
         assert nb.nvfp4_device_error_word() == 0
         ref.assert_product(D[:, :N], *ref.product(a, b), K)
         assert bool((D[:, N:] == 7).all())
+
+
+@pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (3, 5, 9), (129, 131, 257), (300, 1, 40), (700, 1003, 129)])
+def test_products_of_any_size_without_an_output_given(M, N, K, out_dtype):
+    ops, a, b = _operands(M, N, K, M + N)
+    D = nb.nvfp4_gemm_fp8(*ops, out_dtype=out_dtype)
+    assert D.shape == (M, N)
+    ref.assert_product(D, *ref.product(a, b), K)
+    assert nb.nvfp4_device_error_word() == 0
