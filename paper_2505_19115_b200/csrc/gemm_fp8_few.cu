@@ -92,6 +92,10 @@ __device__ __forceinline__ void tc_mma_mxf8(uint32_t d_tmem, uint64_t adesc, uin
                ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(sfa_tmem), "r"(sfb_tmem)
                : "memory");
 }
+// A box on its way into the level-two cache, whatever is written to it until it is loaded.
+__device__ __forceinline__ void prefetch_2d(const CUtensorMap* map, int x, int y) {
+  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
+}
 __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
@@ -179,6 +183,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp8_few_kernel(const __grid_
     uint32_t ph = 0;
     bool ok = true, first = true;
     Item t;
+    if (!p.offsets && issuer && item_at(p, tab, first_item, t))
+      for (int ks = ks0; ks < min(ks1, ks0 + p.stages); ++ks) prefetch_2d(&p.w, ks * kBK, t.n0);
     for (int i = first_item; ok && item_at(p, tab, i, t); i += items_step) {
       const int w_row = t.e * p.N + t.n0;
       const int boxes = (t.rows + p.box - 1) / p.box;
