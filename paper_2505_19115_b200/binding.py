@@ -545,16 +545,9 @@ def nvfp4_quantize_fp8(x, block_rows: int = 1, row: bool = True, transposed: boo
     """FP8 with a power-of-two scale for each block of 128 (block_rows 128: 128 x 128, for weights).  x [rows, cols], or dense
     [batch, rows, cols].  Returns (codes [..., rows, cols], scales, codes_t [..., cols, rows], scales_t), None for what is not wanted;
     scales: linear [..., Rq, ceil(Kq/128)], or a flat swizzled buffer."""
-    shape, stride = x.shape, x.stride()
-    assert x.is_cuda and len(shape) in (2, 3) and stride[-1] == 1 and (len(shape) == 2 or x.is_contiguous())
-    rows, cols = shape[-2:]
-    batch = shape[0] if len(shape) == 3 else 0
-    native = _native()
-    out = native.empty_fp8(x, batch, rows, cols, int(row), int(transposed), sf_layout)
-    # a matrix of one row has no leading dimension to speak of
-    ld = stride[-2] if rows > 1 else max(stride[-2], -(-cols // 8) * 8)
-    st = native.nvfp4_quantize_fp8(x, x, batch or 1, rows, cols, ld, block_rows, *out, sf_layout, stream)
-    _check(st, "nvfp4_quantize_fp8")
+    out = _native().quantize_fp8(x, block_rows, row, transposed, sf_layout, stream)
+    if type(out) is int:
+        raise NvFp4Error(out, "nvfp4_quantize_fp8")
     return out
 
 
@@ -580,10 +573,11 @@ def nvfp4_linear_fp8_fwd(X, W, out=None, out_dtype=torch.float32, workspace=None
     (M, K), N = X.shape, W.shape[0]
     if out is None:
         out = torch.empty((M, N), dtype=out_dtype, device=X.device)
-    assert X.is_contiguous() and W.is_contiguous() and out.is_contiguous() and X.dtype == W.dtype and W.shape[1] == K and out.shape == (M, N)
+    native = _native()
+    assert native.dense(X, None, M, K) and native.dense(W, X, N, K) and native.dense(out, None, M, N)
     if workspace is None:
         workspace = _scratch(nvfp4_linear_fp8_workspace_bytes(M, N, K, FP8_FWD), X.device, None)
-    st = _native().nvfp4_linear_fp8_fwd(X, W, X, M, N, K, out, out, workspace, workspace, stream)
+    st = native.nvfp4_linear_fp8_fwd(X, W, X, M, N, K, out, out, workspace, workspace, stream)
     _check(st, "nvfp4_linear_fp8_fwd")
     return out
 
@@ -595,11 +589,12 @@ def nvfp4_linear_fp8_bwd(dY, W, X, dX=None, dW=None, dx_dtype=torch.float32, dw_
         dX = torch.empty((M, K), dtype=dx_dtype, device=dY.device)
     if dW is None:
         dW = torch.empty((N, K), dtype=dw_dtype, device=dY.device)
-    assert all(t.is_contiguous() for t in (dY, W, X, dX, dW)) and dY.dtype == W.dtype == X.dtype
-    assert W.shape == dW.shape == (N, K) and X.shape == dX.shape == (M, K)
+    native = _native()
+    assert native.dense(dY, None, M, N) and native.dense(W, dY, N, K) and native.dense(X, dY, M, K)
+    assert native.dense(dX, None, M, K) and native.dense(dW, None, N, K)
     if workspace is None:
         workspace = _scratch(nvfp4_linear_fp8_workspace_bytes(M, N, K, FP8_BWD), dY.device, None)
-    st = _native().nvfp4_linear_fp8_bwd(dY, W, X, dY, M, N, K, dX, dX, dW, dW, workspace, workspace, stream)
+    st = native.nvfp4_linear_fp8_bwd(dY, W, X, dY, M, N, K, dX, dX, dW, dW, workspace, workspace, stream)
     _check(st, "nvfp4_linear_fp8_bwd")
     return dX, dW
 
@@ -625,15 +620,16 @@ class ExpertPlan:
 
 def nvfp4_expert_sort(expert_of, experts: int, plan: ExpertPlan = None, stream=None) -> ExpertPlan:
     """Tokens sorted by expert: expert_of [tokens, topk] (int32 or int64; an index outside [0, experts) drops the slot)."""
-    assert expert_of.is_cuda and expert_of.dim() == 2 and expert_of.is_contiguous()
-    if expert_of.dtype not in (torch.int32, torch.int64):
+    wide = expert_of.dtype is torch.int64
+    if not wide and expert_of.dtype is not torch.int32:
         raise TypeError(f"unsupported dtype {expert_of.dtype}")
     tokens, topk = expert_of.shape
+    assert _native().dense(expert_of, None, tokens, topk)
     if plan is None:
         plan = ExpertPlan(tokens, topk, experts, expert_of)
-    assert (plan.tokens, plan.topk, plan.experts) == (tokens, topk, experts)
-    st = _native().nvfp4_expert_sort(expert_of, int(expert_of.dtype == torch.int64), tokens, topk, experts, plan.counts, plan.offsets,
-                                     plan.row_of, plan.slot_of, stream)
+    else:
+        assert (plan.tokens, plan.topk, plan.experts) == (tokens, topk, experts)
+    st = _native().nvfp4_expert_sort(expert_of, int(wide), tokens, topk, experts, plan.counts, plan.offsets, plan.row_of, plan.slot_of, stream)
     _check(st, "nvfp4_expert_sort")
     return plan
 
@@ -642,70 +638,68 @@ def _weights(weights, plan):
     """(tensor or None, its dtype for the call)."""
     if weights is None:
         return None, BF16
-    assert weights.is_contiguous() and weights.shape == (plan.tokens, plan.topk)
+    assert _native().dense(weights, None, plan.tokens, plan.topk)
     return weights, weights
 
 
 def nvfp4_expert_gather(x, plan, weights=None, out=None, stream=None):
     """rows[r] = (weight *) x[token of row r], zero in padding; rows that are not used are left as they are."""
-    assert x.dim() == 2 and x.stride(1) == 1 and x.shape[0] == plan.tokens
-    cols = x.shape[1]
+    native = _native()
+    cols, ld = native.matrix(x, plan.tokens)
     if out is None:
-        out = _native().empty_rows(x, plan.rows, cols)
-    assert out.is_contiguous() and out.shape == (plan.rows, cols) and out.dtype == x.dtype
+        out = native.empty_rows(x, plan.rows, cols)
+    else:
+        assert native.dense(out, x, plan.rows, cols)
     w, w_dtype = _weights(weights, plan)
-    st = _native().nvfp4_expert_gather(x, x, plan.tokens, plan.topk, plan.experts, cols, x.stride(0) if plan.tokens > 1 else cols,
-                                       plan.offsets, plan.slot_of, plan.row_of, w, w_dtype, out, stream)
+    st = native.nvfp4_expert_gather(x, x, plan.tokens, plan.topk, plan.experts, cols, ld, plan.offsets, plan.slot_of, plan.row_of,
+                                    w, w_dtype, out, stream)
     _check(st, "nvfp4_expert_gather")
     return out
 
 
 def nvfp4_expert_combine(rows, plan, weights=None, out=None, stream=None):
     """y[t] = sum_j (weights[t,j] *) rows[row of (t,j)]; without weights the gradient of nvfp4_expert_gather."""
-    assert rows.is_contiguous() and rows.dim() == 2 and rows.shape[0] == plan.rows
-    cols = rows.shape[1]
+    native = _native()
+    cols, _ = native.matrix(rows, plan.rows)
+    assert native.dense(rows, None, plan.rows, cols)
     if out is None:
-        out = _native().empty_rows(rows, plan.tokens, cols)
-    assert out.is_contiguous() and out.shape == (plan.tokens, cols) and out.dtype == rows.dtype
+        out = native.empty_rows(rows, plan.tokens, cols)
+    else:
+        assert native.dense(out, rows, plan.tokens, cols)
     w, w_dtype = _weights(weights, plan)
-    st = _native().nvfp4_expert_combine(rows, rows, plan.tokens, plan.topk, plan.experts, cols, plan.row_of, w, w_dtype, out, stream)
+    st = native.nvfp4_expert_combine(rows, rows, plan.tokens, plan.topk, plan.experts, cols, plan.row_of, w, w_dtype, out, stream)
     _check(st, "nvfp4_expert_combine")
     return out
 
 
 def nvfp4_expert_combine_bwd(dy, rows, plan, weights, rows_gradient: bool = True, drows=None, dweights=None, stream=None):
     """Gradient of nvfp4_expert_combine by its rows and its weights: (drows, or None where it is not wanted; dweights)."""
-    assert dy.dim() == 2 and dy.stride(1) == 1 and dy.shape[0] == plan.tokens and rows.dtype == dy.dtype
-    cols = dy.shape[1]
-    assert rows.is_contiguous() and rows.shape == (plan.rows, cols)
-    if drows is None and rows_gradient:
-        drows = _native().empty_rows(rows, plan.rows, cols)
+    native = _native()
+    cols, ld = native.matrix(dy, plan.tokens)
+    assert native.dense(rows, dy, plan.rows, cols) and native.dense(weights, None, plan.tokens, plan.topk)
+    if drows is not None:
+        assert native.dense(drows, rows, plan.rows, cols)
+    elif rows_gradient:
+        drows = native.empty_rows(rows, plan.rows, cols)
     if dweights is None:
-        dweights = _native().empty_rows(weights, plan.tokens, plan.topk)
-    assert drows is None or (drows.is_contiguous() and drows.shape == rows.shape and drows.dtype == rows.dtype)
-    assert weights.is_contiguous() and dweights.is_contiguous() and dweights.dtype == weights.dtype
-    assert weights.shape == dweights.shape == (plan.tokens, plan.topk)
-    st = _native().nvfp4_expert_combine_bwd(dy, dy, plan.tokens, plan.topk, plan.experts, cols, dy.stride(0) if plan.tokens > 1 else cols,
-                                            plan.offsets, plan.slot_of, plan.row_of, rows, weights, weights, drows, dweights, stream)
+        dweights = native.empty_rows(weights, plan.tokens, plan.topk)
+    else:
+        assert native.dense(dweights, weights, plan.tokens, plan.topk)
+    st = native.nvfp4_expert_combine_bwd(dy, dy, plan.tokens, plan.topk, plan.experts, cols, ld, plan.offsets, plan.slot_of, plan.row_of,
+                                         rows, weights, weights, drows, dweights, stream)
     _check(st, "nvfp4_expert_combine_bwd")
     return drows, dweights
-
-
-def _by_token(x, plan, sorted_rows):
-    assert x.dim() == 2 and x.stride(1) == 1 and x.shape[0] == (plan.rows if sorted_rows else plan.tokens)
-    return int(not sorted_rows)
 
 
 def nvfp4_quantize_fp8_experts(x, plan, weights=None, sorted_rows: bool = False, row: bool = True, transposed: bool = False, stream=None):
     """nvfp4_quantize_fp8 of the sorted rows, gathered on the way from x [tokens, cols] (sorted_rows: x is [rows, cols] already) and
     multiplied by weights.  Returns (codes [rows, cols], scales, codes_t [cols, rows], scales_t)."""
-    by_token = _by_token(x, plan, sorted_rows)
-    cols = x.shape[1]
-    out = _native().empty_fp8(x, 0, plan.rows, cols, int(row), int(transposed), SF_SWIZZLED)
+    native = _native()
+    cols, ld = native.matrix(x, plan.rows if sorted_rows else plan.tokens)
+    out = native.empty_fp8(x, 0, plan.rows, cols, int(row), int(transposed), SF_SWIZZLED)
     w, w_dtype = _weights(weights, plan)
-    ld = x.stride(0) if x.shape[0] > 1 else max(x.stride(0), -(-cols // 8) * 8)
-    st = _native().nvfp4_quantize_fp8_experts(x, x, by_token, plan.tokens, plan.topk, plan.experts, cols, ld, plan.offsets, plan.slot_of,
-                                              w, w_dtype, *out, stream)
+    st = native.nvfp4_quantize_fp8_experts(x, x, int(not sorted_rows), plan.tokens, plan.topk, plan.experts, cols, ld, plan.offsets,
+                                           plan.slot_of, w, w_dtype, *out, stream)
     _check(st, "nvfp4_quantize_fp8_experts")
     return out
 
@@ -744,15 +738,15 @@ def nvfp4_experts_fp8_workspace_bytes(tokens: int, topk: int, experts: int, N: i
 def nvfp4_experts_fp8_fwd(X, W, plan, sorted_rows: bool = False, out=None, out_dtype=None, workspace=None, stream=None):
     """Y[r] = Q(X[r]) . Q(W[e])^T for the rows r of expert e, W [experts, N, K]; X [tokens, K] is gathered on the way (sorted_rows:
     X is [rows, K] already).  Y [rows, N] of X's dtype unless told otherwise."""
-    by_token, (E, N, K) = _by_token(X, plan, sorted_rows), W.shape
+    native, (E, N, K) = _native(), W.shape
     if out is None:
         out = torch.empty((plan.rows, N), dtype=out_dtype or X.dtype, device=X.device)
-    assert X.is_contiguous() and W.is_contiguous() and out.is_contiguous() and X.dtype == W.dtype and X.shape[1] == K
-    assert E == plan.experts and out.shape == (plan.rows, N)
+    assert native.dense(X, W, plan.rows if sorted_rows else plan.tokens, K) and native.dense(W, None, plan.experts, N, K)
+    assert native.dense(out, None, plan.rows, N)
     if workspace is None:
         workspace = _scratch(nvfp4_experts_fp8_workspace_bytes(plan.tokens, plan.topk, E, N, K, FP8_FWD), X.device, None)
-    st = _native().nvfp4_experts_fp8_fwd(X, by_token, W, X, plan.tokens, plan.topk, E, N, K, plan.offsets, plan.slot_of, out, out,
-                                         workspace, workspace, stream)
+    st = native.nvfp4_experts_fp8_fwd(X, int(not sorted_rows), W, X, plan.tokens, plan.topk, E, N, K, plan.offsets, plan.slot_of, out, out,
+                                      workspace, workspace, stream)
     _check(st, "nvfp4_experts_fp8_fwd")
     return out
 
@@ -761,18 +755,18 @@ def nvfp4_experts_fp8_bwd(dY, W, X, plan, weights=None, dy_sorted_rows: bool = F
                           dx_dtype=None, dw_dtype=torch.float32, workspace=None, stream=None):
     """dX [rows, K] and dW [experts, N, K].  dY [tokens, N] is gathered on the way and multiplied by weights, as the gradient of
     nvfp4_expert_combine (dy_sorted_rows: dY is [rows, N] already); X as in nvfp4_experts_fp8_fwd.  Returns (dX, dW)."""
-    dy_by_token, x_by_token, (E, N, K) = _by_token(dY, plan, dy_sorted_rows), _by_token(X, plan, sorted_rows), W.shape
+    native, (E, N, K) = _native(), W.shape
     if dX is None:
         dX = torch.empty((plan.rows, K), dtype=dx_dtype or X.dtype, device=dY.device)
     if dW is None:
         dW = torch.empty((E, N, K), dtype=dw_dtype, device=dY.device)
-    assert all(t.is_contiguous() for t in (dY, W, X, dX, dW)) and dY.dtype == W.dtype == X.dtype
-    assert E == plan.experts and dY.shape[1] == N and X.shape[1] == K and dX.shape == (plan.rows, K) and dW.shape == W.shape
+    assert native.dense(dY, W, plan.rows if dy_sorted_rows else plan.tokens, N) and native.dense(X, W, plan.rows if sorted_rows else plan.tokens, K)
+    assert native.dense(W, None, plan.experts, N, K) and native.dense(dX, None, plan.rows, K) and native.dense(dW, None, E, N, K)
     w, w_dtype = _weights(weights, plan)
     if workspace is None:
         workspace = _scratch(nvfp4_experts_fp8_workspace_bytes(plan.tokens, plan.topk, E, N, K, FP8_BWD), dY.device, None)
-    st = _native().nvfp4_experts_fp8_bwd(dY, dy_by_token, w, w_dtype, W, X, x_by_token, dY, plan.tokens, plan.topk, E, N, K, plan.offsets,
-                                         plan.slot_of, dX, dX, dW, dW, workspace, workspace, stream)
+    st = native.nvfp4_experts_fp8_bwd(dY, int(not dy_sorted_rows), w, w_dtype, W, X, int(not sorted_rows), dY, plan.tokens, plan.topk, E, N, K,
+                                      plan.offsets, plan.slot_of, dX, dX, dW, dW, workspace, workspace, stream)
     _check(st, "nvfp4_experts_fp8_bwd")
     return dX, dW
 

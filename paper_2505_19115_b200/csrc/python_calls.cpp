@@ -22,6 +22,7 @@
 #include <dlfcn.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <tuple>
 #include <type_traits>
 #include <utility>
@@ -210,28 +211,77 @@ PyObject* tuple_of(F&& f) {
   return t;
 }
 
-// empty_fp8(like, batch, rows, cols, row, transposed, sf_layout): (codes [batch, rows, cols], scales, codes_t [batch, cols, rows], scales_t)
-// without the first dimension where batch is 0, None for what is not wanted.  Rows of codes take a multiple of 16 bytes.
+// Codes and scales of both outputs of a quantizer: [batch, rows, cols] and [batch, cols, rows] without the first dimension where batch
+// is 0.  Rows of codes take a multiple of 16 bytes.
+void make_fp8(const at::Tensor& like, int64_t batch, int64_t rows, int64_t cols, const bool (&wanted)[2], int64_t layout, at::Tensor (&out)[4]) {
+  const int64_t size[2] = {rows, cols}, lead = batch ? batch : 1;
+  for (int i = 0; i < 2; ++i) {
+    if (!wanted[i]) continue;
+    const int64_t rq = size[i], kq = size[1 - i], pitch = (kq + 15) / 16 * 16, nb = (kq + 127) / 128;
+    const int64_t whole[3] = {lead, rq, pitch}, part[3] = {lead, rq, kq}, strides[3] = {rq * pitch, pitch, 1}, linear[3] = {lead, rq, nb};
+    const int skip = batch ? 0 : 1;
+    at::Tensor& codes = out[2 * i] = empty(like, at::IntArrayRef(whole).slice(skip), at::kByte);
+    if (pitch != kq) codes.unsafeGetTensorImpl()->set_sizes_and_strides(at::IntArrayRef(part).slice(skip), at::IntArrayRef(strides).slice(skip));
+    out[2 * i + 1] = layout == NVFP4_SF_LINEAR ? empty(like, at::IntArrayRef(linear).slice(skip), at::kByte)
+                                               : empty(like, {lead * ((rq + 127) / 128) * ((nb + 3) / 4) * 512}, at::kByte);
+  }
+}
+int wrap_all(const at::Tensor (&out)[4], PyObject** made) {
+  for (int i = 0; i < 4; ++i)
+    if (out[i].defined()) made[i] = wrap(out[i]);
+  return 4;
+}
+
+// empty_fp8(like, batch, rows, cols, row, transposed, sf_layout): (codes, scales, codes_t, scales_t), None for what is not wanted.
 PyObject* py_empty_fp8(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (n != 7) {
     PyErr_SetString(PyExc_TypeError, "expected 7 arguments");
     return nullptr;
   }
   return tuple_of([&](PyObject** made) {
-    const at::Tensor& like = tensor(args[0]);
-    const int64_t batch = number(args[1]), size[2] = {number(args[2]), number(args[3])}, wanted[2] = {number(args[4]), number(args[5])};
-    const int64_t layout = number(args[6]);
-    for (int i = 0; i < 2; ++i) {
-      if (!wanted[i]) continue;
-      const int64_t rq = size[i], kq = size[1 - i], pitch = (kq + 15) / 16 * 16, nb = (kq + 127) / 128;
-      at::Tensor codes = batch ? empty(like, {batch, rq, pitch}, at::kByte) : empty(like, {rq, pitch}, at::kByte);
-      if (pitch != kq) codes = codes.narrow(-1, 0, kq);
-      made[2 * i] = wrap(codes);
-      if (layout == NVFP4_SF_LINEAR) made[2 * i + 1] = wrap(batch ? empty(like, {batch, rq, nb}, at::kByte) : empty(like, {rq, nb}, at::kByte));
-      else made[2 * i + 1] = wrap(empty(like, {(batch ? batch : 1) * ((rq + 127) / 128) * ((nb + 3) / 4) * 512}, at::kByte));
-    }
-    return 4;
+    const bool wanted[2] = {number(args[4]) != 0, number(args[5]) != 0};
+    at::Tensor out[4];
+    make_fp8(tensor(args[0]), number(args[1]), number(args[2]), number(args[3]), wanted, number(args[6]), out);
+    return wrap_all(out, made);
   });
+}
+// quantize_fp8(x, block_rows, row, transposed, sf_layout, stream): nvfp4_quantize_fp8 of [rows, cols] or of a dense [batch, rows, cols], with
+// outputs as above; or the status that it returned.
+PyObject* py_quantize_fp8(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 6 || !fn_nvfp4_quantize_fp8) {
+    PyErr_SetString(PyExc_TypeError, "expected 6 arguments, after bind()");
+    return nullptr;
+  }
+  int st = 0;
+  PyObject* const made = tuple_of([&](PyObject** made) {
+    const at::Tensor& x = tensor(args[0]);
+    const int64_t d = x.dim();
+    const void* const data = convert_pointer<true, const void*>(args[0]);
+    if ((d != 2 && d != 3) || x.stride(d - 1) != 1 || (d == 3 && !x.is_contiguous())) {
+      PyErr_SetString(PyExc_ValueError, "expected [rows, cols] with dense rows, or a dense [batch, rows, cols]");
+      throw PythonError{};
+    }
+    const int dtype = convert_number<int, true>(args[0]);
+    const int64_t batch = d == 3 ? x.size(0) : 0, rows = x.size(d - 2), cols = x.size(d - 1);
+    const int block_rows = convert_number<int, false>(args[1]), layout = convert_number<int, false>(args[4]);
+    const bool wanted[2] = {number(args[2]) != 0, number(args[3]) != 0};
+    // one row alone has no leading dimension to speak of; matrices of one row lie one behind the other
+    const int64_t ld = rows * std::max<int64_t>(batch, 1) == 1 ? (cols + 7) / 8 * 8 : d == 3 ? cols : x.stride(0);
+    void* const stream = stream_handle(args[5]);
+    at::Tensor out[4];
+    make_fp8(x, batch, rows, cols, wanted, layout, out);
+    uint8_t* to[4];
+    for (int i = 0; i < 4; ++i) to[i] = out[i].defined() ? static_cast<uint8_t*>(out[i].data_ptr()) : nullptr;
+    Py_BEGIN_ALLOW_THREADS
+    st = fn_nvfp4_quantize_fp8(data, dtype, d == 3 ? batch : 1, rows, cols, ld, block_rows, to[0], to[1], to[2], to[3], layout, stream);
+    Py_END_ALLOW_THREADS
+    return wrap_all(out, made);
+  });
+  if (made && st != 0) {
+    Py_DECREF(made);
+    return PyLong_FromLong(st);
+  }
+  return made;
 }
 // expert_buffers(like, tokens, topk, experts, rows): (counts, offsets, row_of, slot_of)
 PyObject* py_expert_buffers(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -242,12 +292,59 @@ PyObject* py_expert_buffers(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return tuple_of([&](PyObject** made) {
     const at::Tensor& like = tensor(args[0]);
     const int64_t tokens = number(args[1]), topk = number(args[2]), experts = number(args[3]), rows = number(args[4]);
-    made[0] = wrap(empty(like, {experts}, at::kInt));
-    made[1] = wrap(empty(like, {experts + 1}, at::kInt));
-    made[2] = wrap(empty(like, {tokens, topk}, at::kInt));
-    made[3] = wrap(empty(like, {rows}, at::kInt));
+    // one buffer; a tensor of its own for each would cost a microsecond
+    const at::Tensor buffer = empty(like, {rows + tokens * topk + 2 * experts + 1}, at::kInt);
+    int64_t at = 0;
+    auto part = [&](std::initializer_list<int64_t> size, int64_t n) {
+      at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(buffer.storage()), buffer.key_set(), buffer.dtype());
+      t.unsafeGetTensorImpl()->set_storage_offset(at);
+      t.unsafeGetTensorImpl()->set_sizes_contiguous(size);
+      at += n;
+      return wrap(t);
+    };
+    made[3] = part({rows}, rows);
+    made[2] = part({tokens, topk}, tokens * topk);
+    made[1] = part({experts + 1}, experts + 1);
+    made[0] = part({experts}, experts);
     return 4;
   });
+}
+// matrix(t, rows): (cols, leading dimension) of [rows, cols] whose rows are dense
+PyObject* py_matrix(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 2) {
+    PyErr_SetString(PyExc_TypeError, "expected 2 arguments");
+    return nullptr;
+  }
+  try {
+    const at::Tensor& t = tensor(args[0]);
+    const int64_t rows = number(args[1]);
+    if (t.dim() != 2 || t.stride(1) != 1 || t.size(0) != rows) {
+      PyErr_Format(PyExc_ValueError, "expected a matrix of %lld dense rows", (long long)rows);
+      return nullptr;
+    }
+    return Py_BuildValue("(LL)", (long long)t.size(1), (long long)(rows > 1 ? t.stride(0) : (t.size(1) + 7) / 8 * 8));
+  } catch (const PythonError&) {
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+  }
+  return nullptr;
+}
+// dense(t, like, size...): whether t is contiguous, of that size, and of the dtype of `like` (None: of any)
+PyObject* py_dense(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n < 2) {
+    PyErr_SetString(PyExc_TypeError, "expected a tensor, another or None, and sizes");
+    return nullptr;
+  }
+  try {
+    const at::Tensor& t = tensor(args[0]);
+    bool yes = t.dim() == n - 2 && t.is_contiguous() && (args[1] == Py_None || t.scalar_type() == tensor(args[1]).scalar_type());
+    for (Py_ssize_t i = 2; yes && i < n; ++i) yes = t.size(i - 2) == number(args[i]);
+    return PyBool_FromLong(yes);
+  } catch (const PythonError&) {
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+  }
+  return nullptr;
 }
 // empty_rows(like, rows, cols): [rows, cols] of like's dtype
 PyObject* py_empty_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -324,6 +421,7 @@ PyObject* py_bind(PyObject*, PyObject* args) {
 #define NVFP4_METHOD(name, ...) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr},
 #define NVFP4_HELPER(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"bind", py_bind, METH_VARARGS, nullptr}, NVFP4_HELPER(empty_fp8), NVFP4_HELPER(expert_buffers), NVFP4_HELPER(empty_rows), NVFP4_HELPER(fp8_operand),
+                         NVFP4_HELPER(quantize_fp8), NVFP4_HELPER(matrix), NVFP4_HELPER(dense),
                          NVFP4_CALLS(NVFP4_METHOD) NVFP4_CALLS_HERE(NVFP4_METHOD){nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

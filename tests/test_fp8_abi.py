@@ -176,3 +176,19 @@ def test_outputs_are_laid_out_as_the_calls_take_them():
             bad()
     with pytest.raises(RuntimeError):
         n.empty_rows(like, -1, 8)
+
+
+def test_shapes_are_read_as_the_calls_take_them():
+    n, t = nb._native(), torch.zeros((6, 40))
+    assert n.matrix(t, 6) == (40, 40) and n.matrix(t[:, :24], 6) == (24, 40) and n.matrix(t[1:2, :12], 1) == (12, 16)
+    for bad in (lambda: n.matrix(t, 5), lambda: n.matrix(t.T, 40), lambda: n.matrix(t[0], 40)):
+        with pytest.raises(ValueError):
+            bad()
+    assert n.dense(t, None, 6, 40) and n.dense(t, t, 6, 40) and n.dense(t.view(2, 3, 40), t, 2, 3, 40)
+    for bad in ((t, None, 6, 41), (t, None, 240), (t, t.half(), 6, 40), (t[:, :8], None, 6, 8), (t.T, None, 40, 6)):
+        assert not n.dense(*bad)
+    for bad in (lambda: n.matrix(t), lambda: n.matrix(5, 6), lambda: n.dense(t), lambda: n.dense(None, None, 1), lambda: n.dense(t, 5, 6, 40)):
+        with pytest.raises(TypeError):
+            bad()
+    with pytest.raises((ValueError, RuntimeError)):                   # a host tensor; RuntimeError: no CUDA device to be current
+        nb.nvfp4_quantize_fp8(torch.zeros((8, 8)))

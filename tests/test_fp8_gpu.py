@@ -297,3 +297,18 @@ def test_products_of_any_size_without_an_output_given(M, N, K, out_dtype):
     assert D.shape == (M, N)
     ref.assert_product(D, *ref.product(a, b), K)
     assert nb.nvfp4_device_error_word() == 0
+
+
+def test_quantizer_of_single_rows_wherever_they_lie():
+    whole = _x((6, 44), 3)
+    for x in (whole[2:3, 8:20], whole[1:2, :44], whole[4:5, 16:24]):             # strides that say nothing, and are no multiple of 8
+        if x.data_ptr() % 16 == 0:
+            _check_quantized(x, 1, nb.SF_LINEAR, *nb.nvfp4_quantize_fp8(x, transposed=True, sf_layout=nb.SF_LINEAR))
+    batch = _x((3, 1, 24), 4)
+    codes, scales, _, _ = nb.nvfp4_quantize_fp8(batch, sf_layout=nb.SF_LINEAR)
+    for i in range(3):
+        one = nb.nvfp4_quantize_fp8(batch[i], sf_layout=nb.SF_LINEAR)
+        assert torch.equal(codes[i], one[0]) and torch.equal(scales[i], one[1])
+    with pytest.raises(nb.NvFp4Error):                                            # the next matrix would begin inside a vector
+        nb.nvfp4_quantize_fp8(_x((3, 1, 12), 5))
+    nb.nvfp4_quantize_fp8(_x((1, 1, 12), 5))
