@@ -81,6 +81,8 @@ struct Fp8Product {
 int gemm_fp8(const Fp8Product& p, cudaStream_t s);
 // The same for few rows (gemm_fp8_few.cu): one product, or by rows with their counts.  Padding rows of D are not written.
 int gemm_fp8_few(const Fp8Product& p, cudaStream_t s);
+// Two products of which the second needs nothing of the first's.
+int gemm_fp8_two(const Fp8Product& a, const Fp8Product& b, cudaStream_t s);
 int fp8_error_word(unsigned int* out);
 int fp8_few_error_word(unsigned int* out);
 

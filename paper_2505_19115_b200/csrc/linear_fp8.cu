@@ -98,10 +98,8 @@ extern "C" int nvfp4_linear_fp8_bwd(const void* dY, const void* W, const void* X
                              {X, 1, M, K, K, 0, nullptr, nullptr, ws + l.xt.codes, ws + l.xt.sf, {}},
                              {dY, 1, M, N, N, 0, ws + l.dy.codes, ws + l.dy.sf, ws + l.dyt.codes, ws + l.dyt.sf, {}}};
   if (int st = quantize_fp8(ops, 3, dtype, NVFP4_SF_SWIZZLED_128x4, s)) return st;
-  if (int st = gemm_fp8({ws + l.dy.codes, ws + l.dy.sf, ws + l.wt.codes, ws + l.wt.sf, M, K, N, dX, dx_dtype, K}, s)) return st;
-  Fp8Product dw = {ws + l.dyt.codes, ws + l.dyt.sf, ws + l.xt.codes, ws + l.xt.sf, N, K, M, dW, dw_dtype, K};
-  dw.late = true;                                        // it does not depend on dX, and begins where multiprocessors are done with that
-  return gemm_fp8(dw, s);
+  return gemm_fp8_two({ws + l.dy.codes, ws + l.dy.sf, ws + l.wt.codes, ws + l.wt.sf, M, K, N, dX, dx_dtype, K},
+                      {ws + l.dyt.codes, ws + l.dyt.sf, ws + l.xt.codes, ws + l.xt.sf, N, K, M, dW, dw_dtype, K}, s);
 }
 
 extern "C" size_t nvfp4_experts_fp8_workspace_bytes(int64_t tokens, int64_t topk, int64_t experts, int64_t N, int64_t K, int which) {
@@ -171,10 +169,7 @@ extern "C" int nvfp4_experts_fp8_bwd(const void* dY, int dy_by_token, const void
                              {X, 1, R, K, K, 0, nullptr, nullptr, ws + l.xt.codes, ws + l.xt.sf, x_from},
                              {dY, 1, R, N, N, 0, ws + l.dy.codes, ws + l.dy.sf, ws + l.dyt.codes, ws + l.dyt.sf, dy_from}};
   if (int st = quantize_fp8(ops, 3, dtype, NVFP4_SF_SWIZZLED_128x4, s)) return st;
-  if (int st = gemm_fp8({ws + l.dy.codes, ws + l.dy.sf, ws + l.wt.codes, ws + l.wt.sf, R, K, N, dX, dx_dtype, K, experts, offsets, true, nullptr,
-                         tokens * topk}, s))
-    return st;
-  Fp8Product dw = {ws + l.dyt.codes, ws + l.dyt.sf, ws + l.xt.codes, ws + l.xt.sf, N, K, R, dW, dw_dtype, K, experts, offsets, false};
-  dw.late = true;
-  return gemm_fp8(dw, s);
+  return gemm_fp8_two({ws + l.dy.codes, ws + l.dy.sf, ws + l.wt.codes, ws + l.wt.sf, R, K, N, dX, dx_dtype, K, experts, offsets, true, nullptr,
+                       tokens * topk},
+                      {ws + l.dyt.codes, ws + l.dyt.sf, ws + l.xt.codes, ws + l.xt.sf, N, K, R, dW, dw_dtype, K, experts, offsets, false}, s);
 }

@@ -312,3 +312,22 @@ def test_quantizer_of_single_rows_wherever_they_lie():
     with pytest.raises(nb.NvFp4Error):                                            # the next matrix would begin inside a vector
         nb.nvfp4_quantize_fp8(_x((3, 1, 12), 5))
     nb.nvfp4_quantize_fp8(_x((1, 1, 12), 5))
+
+
+@pytest.mark.parametrize("dx_dtype,dw_dtype", [(torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32)])
+@pytest.mark.parametrize("shape", [(129, 136, 136), (256, 512, 512), (777, 1000, 1160), (700, 704, 2048), (1024, 1024, 2048), (1000, 1400, 1536),
+                                   (1024, 1600, 2048), (129, 9472, 8), (200, 136, 12296)])
+def test_gradients_of_one_launch_are_those_of_two(shape, dx_dtype, dw_dtype):
+    # every tile with a pair of its own, in each width; more tiles than pairs; a contraction too long for it; few rows
+    M, N, K = shape
+    X, W, dY = _x((M, K), 1), _x((N, K), 2), _x((M, N), 3)
+    want_dx, want_dw = (torch.empty(s, dtype=t, device="cuda") for s, t in (((M, K), dx_dtype), ((N, K), dw_dtype)))
+    _, _, wt, wts = nb.nvfp4_quantize_fp8(W, 128, False, True)
+    _, _, xt, xts = nb.nvfp4_quantize_fp8(X, 1, False, True)
+    dy, dys, dyt, dyts = nb.nvfp4_quantize_fp8(dY, 1, True, True)
+    nb.nvfp4_gemm_fp8(dy, dys, wt, wts, out=want_dx)
+    nb.nvfp4_gemm_fp8(dyt, dyts, xt, xts, out=want_dw)
+    for _ in range(3):
+        dX, dW = nb.nvfp4_linear_fp8_bwd(dY, W, X, dx_dtype=dx_dtype, dw_dtype=dw_dtype)
+        assert torch.equal(dX, want_dx) and torch.equal(dW, want_dw)
+    assert nb.nvfp4_device_error_word() == 0
