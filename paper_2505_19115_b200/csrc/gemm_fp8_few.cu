@@ -183,6 +183,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp8_few_kernel(const __grid_
     uint32_t ph = 0;
     bool ok = true, first = true;
     Item t;
+    // One product knows its first weights before the kernel ahead is done, the quantizer of its rows as a rule: into the level-two cache,
+    // which that kernel's writes go through as well, they may come early (both calls, 11008 x 4096 and one row: 15.5 -> 15.2 us).
     if (!p.offsets && issuer && item_at(p, tab, first_item, t))
       for (int ks = ks0; ks < min(ks1, ks0 + p.stages); ++ks) prefetch_2d(&p.w, ks * kBK, t.n0);
     for (int i = first_item; ok && item_at(p, tab, i, t); i += items_step) {
