@@ -7,6 +7,10 @@ or a call fails, an exception is raised.
 
 The calls that launch work go through the extension module _calls (csrc/python_calls.cpp says how it takes its
 arguments), the queries through ctypes.
+
+A call that is given a stream runs there, and what it allocates is that stream's: its scratch, and the outputs that are
+not given.  They may be passed on to further calls on that stream and dropped at any time; the caller lets the streams
+wait for one another as for any tensor.
 """
 import ctypes as C
 import functools
@@ -205,6 +209,22 @@ def _stream(stream=None):
     return _raw_stream(torch.cuda.current_device())
 
 
+def _empty(size, dtype, like, stream):
+    """An output of a call on `stream` (None: the current stream), on the device of the tensor `like`."""
+    if stream is None:
+        return torch.empty(size, dtype=dtype, device=like.device)
+    return _native().empty_on(stream, like, dtype, 1, *size)
+
+
+def _scratch(nbytes, like, given, stream):
+    """The workspace of a call on `stream`: `given`, or one that nothing else uses before the call's kernels are done with it."""
+    if given is not None:
+        return given
+    if stream is None:
+        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=like.device)
+    return _native().empty_on(stream, like, torch.uint8, 0, max(nbytes, 256))
+
+
 def nvfp4_sf_bytes(Rq: int, Kq: int, sf_layout: int = SF_SWIZZLED) -> int:
     return int(lib().nvfp4_sf_bytes(Rq, Kq, sf_layout))
 
@@ -218,12 +238,12 @@ def nvfp4_quantize(x: torch.Tensor, transposed: bool = False, global_scale: torc
     Rq, Kq = (cols, rows) if transposed else (rows, cols)
     rounding = rounding or Rounding()
     if codes is None:
-        codes = torch.empty((Rq, max(Kq // 2, 1)), dtype=torch.uint8, device=x.device)
+        codes = _empty((Rq, max(Kq // 2, 1)), torch.uint8, x, stream)
     if scales is None:
         if sf_layout == SF_LINEAR:
-            scales = torch.empty((Rq, max(Kq // 16, 1)), dtype=torch.uint8, device=x.device)
+            scales = _empty((Rq, max(Kq // 16, 1)), torch.uint8, x, stream)
         else:
-            scales = torch.empty(max(nvfp4_sf_bytes(Rq, Kq, sf_layout), 16), dtype=torch.uint8, device=x.device)
+            scales = _empty((max(nvfp4_sf_bytes(Rq, Kq, sf_layout), 16),), torch.uint8, x, stream)
     st = _native().nvfp4_quantize(x, x, rows, cols, x.stride(0), int(transposed), global_scale, rounding, codes, scales,
                                   sf_layout, stream)
     _check(st, "nvfp4_quantize")
@@ -239,10 +259,10 @@ def nvfp4_quantize_dual(x: torch.Tensor, global_scale: torch.Tensor = None, roun
     rounding_t = rounding_t or Rounding()
 
     def bufs(Rq, Kq):
-        codes = torch.empty((Rq, max(Kq // 2, 1)), dtype=torch.uint8, device=x.device)
+        codes = _empty((Rq, max(Kq // 2, 1)), torch.uint8, x, stream)
         if sf_layout == SF_LINEAR:
-            return codes, torch.empty((Rq, max(Kq // 16, 1)), dtype=torch.uint8, device=x.device)
-        return codes, torch.empty(max(nvfp4_sf_bytes(Rq, Kq, sf_layout), 16), dtype=torch.uint8, device=x.device)
+            return codes, _empty((Rq, max(Kq // 16, 1)), torch.uint8, x, stream)
+        return codes, _empty((max(nvfp4_sf_bytes(Rq, Kq, sf_layout), 16),), torch.uint8, x, stream)
 
     cr, sr = bufs(rows, cols)
     ct, stt = bufs(cols, rows)
@@ -256,7 +276,7 @@ def nvfp4_quantization_noise(x: torch.Tensor, codes, scales, transposed: bool = 
                              sf_layout: int = SF_LINEAR, stream=None) -> torch.Tensor:
     """Device tensor of two doubles: sum (Q(x) - x)^2 and sum x^2 (Section 4's noise and norm)."""
     assert x.is_cuda and x.dim() == 2 and x.stride(1) == 1
-    sums = torch.empty(2, dtype=torch.float64, device=x.device)
+    sums = _empty((2,), torch.float64, x, stream)
     st = lib().nvfp4_quantization_noise(_ptr(x), _dtype_code(x), x.shape[0], x.shape[1], x.stride(0), int(transposed),
                                         _ptr(global_scale), _ptr(codes), _ptr(scales), sf_layout, _ptr(sums),
                                         _stream(stream))
@@ -267,7 +287,7 @@ def nvfp4_quantization_noise(x: torch.Tensor, codes, scales, transposed: bool = 
 def nvfp4_tensor_amax_scale(x: torch.Tensor, out: torch.Tensor = None, stream=None) -> torch.Tensor:
     assert x.is_cuda and x.dim() == 2 and x.stride(1) == 1
     if out is None:
-        out = torch.empty(1, dtype=torch.float32, device=x.device)
+        out = _empty((1,), torch.float32, x, stream)
     st = _native().nvfp4_tensor_amax_scale(x, x, x.shape[0], x.shape[1], x.stride(0), out, stream)
     _check(st, "nvfp4_tensor_amax_scale")
     return out
@@ -279,7 +299,7 @@ def nvfp4_gemm(a_codes, a_sf, a_g, b_codes, b_sf, b_g, out_dtype=torch.float32, 
     M, K = a_codes.shape[0], a_codes.shape[1] * 2
     N = b_codes.shape[0]
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype, device=a_codes.device)
+        out = _empty((M, N), out_dtype, a_codes, stream)
     st = _native().nvfp4_gemm(a_codes, a_sf, a_g, b_codes, b_sf, b_g, M, N, K, out, out, out.stride(0), stream)
     _check(st, "nvfp4_gemm")
     return out
@@ -291,11 +311,11 @@ def nvfp4_gemm_quantized(a_codes, a_sf, a_g, b_codes, b_sf, b_g, out_global_scal
     M, K = a_codes.shape[0], a_codes.shape[1] * 2
     N = b_codes.shape[0]
     rounding = rounding or Rounding()
-    codes = torch.empty((M, N // 2), dtype=torch.uint8, device=a_codes.device)
+    codes = _empty((M, N // 2), torch.uint8, a_codes, stream)
     if sf_layout == SF_LINEAR:
-        scales = torch.empty((M, N // 16), dtype=torch.uint8, device=a_codes.device)
+        scales = _empty((M, N // 16), torch.uint8, a_codes, stream)
     else:
-        scales = torch.empty(max(nvfp4_sf_bytes(M, N, sf_layout), 16), dtype=torch.uint8, device=a_codes.device)
+        scales = _empty((max(nvfp4_sf_bytes(M, N, sf_layout), 16),), torch.uint8, a_codes, stream)
     st = _native().nvfp4_gemm_quantized(a_codes, a_sf, a_g, b_codes, b_sf, b_g, M, N, K, out_global_scale, rounding,
                                         codes, scales, sf_layout, stream)
     _check(st, "nvfp4_gemm_quantized")
@@ -312,9 +332,9 @@ def nvfp4_linear_workspace_bytes(M: int, N: int, K: int, which: int) -> int:
 
 def _linear(name, which, a, b, M, N, K, out_shape, gscale_mode, ga, gb, ra, rb, out, out_dtype, workspace, stream):
     if out is None:
-        out = torch.empty(out_shape, dtype=out_dtype, device=a.device)
+        out = _empty(out_shape, out_dtype, a, stream)
     if workspace is None:
-        workspace = torch.empty(nvfp4_linear_workspace_bytes(M, N, K, which), dtype=torch.uint8, device=a.device)
+        workspace = _scratch(nvfp4_linear_workspace_bytes(M, N, K, which), a, None, stream)
     assert a.is_contiguous() and b.is_contiguous() and out.is_contiguous() and a.dtype == b.dtype
     st = getattr(_native(), name)(a, b, a, M, N, K, gscale_mode, ga, gb, ra, rb, out, out, workspace, workspace, stream)
     _check(st, name)
@@ -350,14 +370,14 @@ def nvfp4_linear_fwd_qout(X, W, gy=None, ry=None, gscale_mode=G_AMAX, gx=None, g
     """Forward layer whose output leaves the GEMM already quantized along N: returns (codes [M, N/2], scales)."""
     (M, K), N = X.shape, W.shape[0]
     if codes is None:
-        codes = torch.empty((M, N // 2), dtype=torch.uint8, device=X.device)
+        codes = _empty((M, N // 2), torch.uint8, X, stream)
     if scales is None:
         if sf_layout == SF_LINEAR:
-            scales = torch.empty((M, N // 16), dtype=torch.uint8, device=X.device)
+            scales = _empty((M, N // 16), torch.uint8, X, stream)
         else:
-            scales = torch.empty(max(nvfp4_sf_bytes(M, N, sf_layout), 16), dtype=torch.uint8, device=X.device)
+            scales = _empty((max(nvfp4_sf_bytes(M, N, sf_layout), 16),), torch.uint8, X, stream)
     if workspace is None:
-        workspace = torch.empty(nvfp4_linear_workspace_bytes(M, N, K, LINEAR_FWD), dtype=torch.uint8, device=X.device)
+        workspace = _scratch(nvfp4_linear_workspace_bytes(M, N, K, LINEAR_FWD), X, None, stream)
     assert X.is_contiguous() and W.is_contiguous() and X.dtype == W.dtype
     st = _native().nvfp4_linear_fwd_qout(X, W, X, M, N, K, gscale_mode, gx, gw, rx or Rounding(RTN),
                                          rw or Rounding(RTN), gy, ry or Rounding(RTN), codes, scales, sf_layout,
@@ -372,9 +392,9 @@ def nvfp4_linear_fwd_qin(x_codes, x_scales, gx, W, gscale_mode=G_AMAX, gw=None, 
     M, K = x_codes.shape[0], x_codes.shape[1] * 2
     N = W.shape[0]
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype, device=W.device)
+        out = _empty((M, N), out_dtype, W, stream)
     if workspace is None:
-        workspace = torch.empty(nvfp4_linear_workspace_bytes(M, N, K, LINEAR_FWD), dtype=torch.uint8, device=W.device)
+        workspace = _scratch(nvfp4_linear_workspace_bytes(M, N, K, LINEAR_FWD), W, None, stream)
     assert W.is_contiguous() and out.is_contiguous()
     st = _native().nvfp4_linear_fwd_qin(x_codes, x_scales, gx, W, W, M, N, K, gscale_mode, gw, rw or Rounding(RTN), out,
                                         out, workspace, workspace, stream)
@@ -393,21 +413,16 @@ def nvfp4_linear_fused_workspace_bytes(M, N, K, which) -> int:
     return int(lib().nvfp4_linear_fused_workspace_bytes(M, N, K, which))
 
 
-def _scratch(nbytes, device, given):
-    if given is not None:
-        return given
-    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
-
-
 def nvfp4_linear_fwd_save(X, W, gscale_mode=G_AMAX, gx=None, gw=None, rx=None, rw=None, rxt=None, rwt=None, out=None,
                           out_dtype=torch.float32, saved=None, workspace=None, stream=None):
     """Y = Q(X) . Q(W)^T and, from the same reads, Q(X^T) and Q(W^T) into `saved` for the backward
     and update passes.  Returns (Y, saved).  Default rounding: the paper's (RtN, RtN, SR for X^T, RtN for W^T)."""
     (M, K), N = X.shape, W.shape[0]
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype, device=X.device)
-    saved = _scratch(nvfp4_linear_saved_bytes(M, N, K), X.device, saved)
-    ws = _scratch(nvfp4_linear_fused_workspace_bytes(M, N, K, FUSED_FWD_SAVE), X.device, workspace)
+        out = _empty((M, N), out_dtype, X, stream)
+    if saved is None:
+        saved = _empty((max(nvfp4_linear_saved_bytes(M, N, K), 256),), torch.uint8, X, stream)
+    ws = _scratch(nvfp4_linear_fused_workspace_bytes(M, N, K, FUSED_FWD_SAVE), X, workspace, stream)
     st = _native().nvfp4_linear_fwd_save(X, W, X, M, N, K, gscale_mode, gx, gw, rx or Rounding(RTN),
                                          rw or Rounding(RTN), rxt or Rounding(SR, 0, 2), rwt or Rounding(RTN), out, out,
                                          saved, saved, ws, ws, stream)
@@ -420,10 +435,10 @@ def nvfp4_linear_bwd_saved(dY, saved, K, gscale_mode=G_AMAX, gdy=None, rdy=None,
     """dX and dW from one read of dY and the operands nvfp4_linear_fwd_save kept.  Returns (dX, dW)."""
     M, N = dY.shape
     if dX is None:
-        dX = torch.empty((M, K), dtype=dx_dtype, device=dY.device)
+        dX = _empty((M, K), dx_dtype, dY, stream)
     if dW is None:
-        dW = torch.empty((N, K), dtype=dw_dtype, device=dY.device)
-    ws = _scratch(nvfp4_linear_fused_workspace_bytes(M, N, K, FUSED_BWD_SAVED), dY.device, workspace)
+        dW = _empty((N, K), dw_dtype, dY, stream)
+    ws = _scratch(nvfp4_linear_fused_workspace_bytes(M, N, K, FUSED_BWD_SAVED), dY, workspace, stream)
     st = _native().nvfp4_linear_bwd_saved(dY, dY, M, N, K, gscale_mode, gdy, rdy or Rounding(SR, 0, 0),
                                           rdyt or Rounding(SR, 0, 1), saved, saved, dX, dX, dW, dW, ws, ws, stream)
     _check(st, "nvfp4_linear_bwd_saved")
@@ -435,10 +450,10 @@ def nvfp4_linear_bwd(dY, W, X, gscale_mode=G_AMAX, gdy=None, gw=None, gx=None, r
     """dX and dW (Eq. 2/5 and Eq. 3/6) with dY read once.  Returns (dX, dW)."""
     (M, N), K = dY.shape, W.shape[1]
     if dX is None:
-        dX = torch.empty((M, K), dtype=dx_dtype, device=dY.device)
+        dX = _empty((M, K), dx_dtype, dY, stream)
     if dW is None:
-        dW = torch.empty((N, K), dtype=dw_dtype, device=dY.device)
-    ws = _scratch(nvfp4_linear_fused_workspace_bytes(M, N, K, FUSED_BWD), dY.device, workspace)
+        dW = _empty((N, K), dw_dtype, dY, stream)
+    ws = _scratch(nvfp4_linear_fused_workspace_bytes(M, N, K, FUSED_BWD), dY, workspace, stream)
     st = _native().nvfp4_linear_bwd(dY, W, X, dY, M, N, K, gscale_mode, gdy, gw, gx, rdy or Rounding(SR, 0, 0),
                                     rdyt or Rounding(SR, 0, 1), rwt or Rounding(RTN), rxt or Rounding(SR, 0, 2), dX, dX,
                                     dW, dW, ws, ws, stream)
@@ -457,17 +472,17 @@ def nvfp4_quantize_mx(x, transposed: bool = False, global_scale=None, rounding: 
     rows, cols = x.shape
     Rq, Kq = (cols, rows) if transposed else (rows, cols)
     rounding = rounding or Rounding()
-    codes = torch.empty((Rq, Kq // 2), dtype=torch.uint8, device=x.device)
+    codes = _empty((Rq, Kq // 2), torch.uint8, x, stream)
     if sf_layout == SF_LINEAR:
-        scales = torch.empty((Rq, Kq // 32), dtype=torch.uint8, device=x.device)
+        scales = _empty((Rq, Kq // 32), torch.uint8, x, stream)
     else:
-        scales = torch.empty(max(nvfp4_sf_bytes_mx(Rq, Kq, sf_layout), 16), dtype=torch.uint8, device=x.device)
+        scales = _empty((max(nvfp4_sf_bytes_mx(Rq, Kq, sf_layout), 16),), torch.uint8, x, stream)
     def call(ws):
         return _native().nvfp4_quantize_mx(x, x, rows, cols, x.stride(0), int(transposed), global_scale, rounding,
                                            codes, scales, sf_layout, ws, ws.numel() if ws is not None else 0, stream)
     st = call(None)
     if st == 5 and transposed:          # a shape the tile kernel does not take: the library transposes into a workspace first
-        st = call(torch.empty(rows * cols * 2, dtype=torch.uint8, device=x.device))
+        st = call(_scratch(rows * cols * 2, x, None, stream))
     _check(st, "nvfp4_quantize_mx")
     return codes, scales
 
@@ -477,7 +492,7 @@ def nvfp4_gemm_mx(a_codes, a_sf, a_g, b_codes, b_sf, b_g, out_dtype=torch.float3
     M, K = a_codes.shape[0], a_codes.shape[1] * 2
     N = b_codes.shape[0]
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype, device=a_codes.device)
+        out = _empty((M, N), out_dtype, a_codes, stream)
     st = _native().nvfp4_gemm_mx(a_codes, a_sf, a_g, b_codes, b_sf, b_g, M, N, K, out, out, out.stride(0), stream)
     _check(st, "nvfp4_gemm_mx")
     return out
@@ -488,7 +503,7 @@ def nvfp4_gemm_bf16(A, B, out_dtype=torch.float32, out=None, stream=None):
     assert A.dtype == torch.bfloat16 and B.dtype == torch.bfloat16 and A.is_contiguous() and B.is_contiguous()
     (M, K), N = A.shape, B.shape[0]
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype, device=A.device)
+        out = _empty((M, N), out_dtype, A, stream)
     _check(_native().nvfp4_gemm_bf16(A, B, M, N, K, out, out, out.stride(0), stream), "nvfp4_gemm_bf16")
     return out
 
@@ -499,7 +514,7 @@ def nvfp4_gemm_bf16_ex(A, a_mn_major, B, b_mn_major, out_dtype=torch.float32, ou
     (K, M) = A.shape if a_mn_major else A.shape[::-1]
     N = B.shape[1] if b_mn_major else B.shape[0]
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype, device=A.device)
+        out = _empty((M, N), out_dtype, A, stream)
     _check(_native().nvfp4_gemm_bf16_ex(A, int(a_mn_major), B, int(b_mn_major), M, N, K, out, out, out.stride(0),
                                         stream), "nvfp4_gemm_bf16_ex")
     return out
@@ -507,7 +522,7 @@ def nvfp4_gemm_bf16_ex(A, a_mn_major, B, b_mn_major, out_dtype=torch.float32, ou
 
 def nvfp4_transpose_bf16(x, stream=None):
     assert x.dtype == torch.bfloat16 and x.dim() == 2 and x.stride(1) == 1
-    out = torch.empty((x.shape[1], x.shape[0]), dtype=torch.bfloat16, device=x.device)
+    out = _empty((x.shape[1], x.shape[0]), torch.bfloat16, x, stream)
     _check(lib().nvfp4_transpose_bf16(_ptr(x), x.shape[0], x.shape[1], x.stride(0), _ptr(out), _stream(stream)),
            "nvfp4_transpose_bf16")
     return out
@@ -516,9 +531,9 @@ def nvfp4_transpose_bf16(x, stream=None):
 def nvfp4_linear_bwd_bf16(dY, W, X, dx_dtype=torch.float32, dw_dtype=torch.float32, workspace=None, stream=None):
     """QAF backward + update in BF16: returns (dX[M,K], dW[N,K])."""
     (M, N), K = dY.shape, W.shape[1]
-    dX = torch.empty((M, K), dtype=dx_dtype, device=dY.device)
-    dW = torch.empty((N, K), dtype=dw_dtype, device=dY.device)
-    ws = _scratch(int(lib().nvfp4_linear_bwd_bf16_workspace_bytes(M, N, K)), dY.device, workspace)
+    dX = _empty((M, K), dx_dtype, dY, stream)
+    dW = _empty((N, K), dw_dtype, dY, stream)
+    ws = _scratch(int(lib().nvfp4_linear_bwd_bf16_workspace_bytes(M, N, K)), dY, workspace, stream)
     _check(_native().nvfp4_linear_bwd_bf16(dY, W, X, M, N, K, dX, dX, dW, dW, ws, ws, stream), "nvfp4_linear_bwd_bf16")
     return dX, dW
 
@@ -534,10 +549,10 @@ def nvfp4_sf_bytes_fp8(Rq: int, Kq: int, sf_layout: int = SF_SWIZZLED) -> int:
     return int(lib().nvfp4_sf_bytes_fp8(Rq, Kq, sf_layout))
 
 
-def _product_rows(M, N, dtype, device):
+def _product_rows(M, N, dtype, like, stream):
     """[M, N] with rows of a multiple of 16 bytes."""
     whole = 16 // dtype.itemsize
-    out = torch.empty((M, -(-N // whole) * whole), dtype=dtype, device=device)
+    out = _empty((M, -(-N // whole) * whole), dtype, like, stream)
     return out if N % whole == 0 else out[:, :N]
 
 
@@ -557,7 +572,7 @@ def nvfp4_gemm_fp8(a_codes, a_sf, b_codes, b_sf, out_dtype=torch.float32, out=No
     (a, M, K), (b, N, Kb) = native.fp8_operand(a_codes, a_sf), native.fp8_operand(b_codes, b_sf)
     assert K == Kb and a == b == 1
     if out is None:
-        out = _product_rows(M, N, out_dtype, a_codes.device)
+        out = _product_rows(M, N, out_dtype, a_codes, stream)
     assert out.shape == (M, N) and out.stride(1) == 1
     st = native.nvfp4_gemm_fp8(a_codes, a_sf, b_codes, b_sf, M, N, K, out, out, out.stride(0), stream)
     _check(st, "nvfp4_gemm_fp8")
@@ -572,11 +587,11 @@ def nvfp4_linear_fp8_fwd(X, W, out=None, out_dtype=torch.float32, workspace=None
     """Y[M,N] = Q(X) . Q(W)^T (Eq. 1) in FP8: blocks of 1 x 128 for X, 128 x 128 for W."""
     (M, K), N = X.shape, W.shape[0]
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype, device=X.device)
+        out = _empty((M, N), out_dtype, X, stream)
     native = _native()
     assert native.dense(X, None, M, K) and native.dense(W, X, N, K) and native.dense(out, None, M, N)
     if workspace is None:
-        workspace = _scratch(nvfp4_linear_fp8_workspace_bytes(M, N, K, FP8_FWD), X.device, None)
+        workspace = _scratch(nvfp4_linear_fp8_workspace_bytes(M, N, K, FP8_FWD), X, None, stream)
     st = native.nvfp4_linear_fp8_fwd(X, W, X, M, N, K, out, out, workspace, workspace, stream)
     _check(st, "nvfp4_linear_fp8_fwd")
     return out
@@ -586,14 +601,14 @@ def nvfp4_linear_fp8_bwd(dY, W, X, dX=None, dW=None, dx_dtype=torch.float32, dw_
     """dX[M,K] and dW[N,K] (Eq. 2-3) in FP8, every tensor read once.  Returns (dX, dW)."""
     (M, N), K = dY.shape, W.shape[1]
     if dX is None:
-        dX = torch.empty((M, K), dtype=dx_dtype, device=dY.device)
+        dX = _empty((M, K), dx_dtype, dY, stream)
     if dW is None:
-        dW = torch.empty((N, K), dtype=dw_dtype, device=dY.device)
+        dW = _empty((N, K), dw_dtype, dY, stream)
     native = _native()
     assert native.dense(dY, None, M, N) and native.dense(W, dY, N, K) and native.dense(X, dY, M, K)
     assert native.dense(dX, None, M, K) and native.dense(dW, None, N, K)
     if workspace is None:
-        workspace = _scratch(nvfp4_linear_fp8_workspace_bytes(M, N, K, FP8_BWD), dY.device, None)
+        workspace = _scratch(nvfp4_linear_fp8_workspace_bytes(M, N, K, FP8_BWD), dY, None, stream)
     st = native.nvfp4_linear_fp8_bwd(dY, W, X, dY, M, N, K, dX, dX, dW, dW, workspace, workspace, stream)
     _check(st, "nvfp4_linear_fp8_bwd")
     return dX, dW
@@ -609,13 +624,13 @@ class ExpertPlan:
     slot_of [rows], int32 on the device."""
     __slots__ = ("tokens", "topk", "experts", "rows", "counts", "offsets", "row_of", "slot_of")
 
-    def __init__(self, tokens, topk, experts, like):
-        """Buffers on the device of the tensor `like`, not filled."""
+    def __init__(self, tokens, topk, experts, like, stream=None):
+        """Buffers on the device of the tensor `like`, not filled; stream: that of the call that fills them."""
         self.tokens, self.topk, self.experts = tokens, topk, experts
         self.rows = nvfp4_expert_rows(tokens, topk, experts)
         if self.rows == 0:
             raise NvFp4Error(2, "nvfp4_expert_rows")
-        self.counts, self.offsets, self.row_of, self.slot_of = _native().expert_buffers(like, tokens, topk, experts, self.rows)
+        self.counts, self.offsets, self.row_of, self.slot_of = _native().expert_buffers(like, tokens, topk, experts, self.rows, stream)
 
 
 def nvfp4_expert_sort(expert_of, experts: int, plan: ExpertPlan = None, stream=None) -> ExpertPlan:
@@ -626,7 +641,7 @@ def nvfp4_expert_sort(expert_of, experts: int, plan: ExpertPlan = None, stream=N
     tokens, topk = expert_of.shape
     assert _native().dense(expert_of, None, tokens, topk)
     if plan is None:
-        plan = ExpertPlan(tokens, topk, experts, expert_of)
+        plan = ExpertPlan(tokens, topk, experts, expert_of, stream)
     else:
         assert (plan.tokens, plan.topk, plan.experts) == (tokens, topk, experts)
     st = _native().nvfp4_expert_sort(expert_of, int(wide), tokens, topk, experts, plan.counts, plan.offsets, plan.row_of, plan.slot_of, stream)
@@ -647,7 +662,7 @@ def nvfp4_expert_gather(x, plan, weights=None, out=None, stream=None):
     native = _native()
     cols, ld = native.matrix(x, plan.tokens)
     if out is None:
-        out = native.empty_rows(x, plan.rows, cols)
+        out = native.empty_rows(x, plan.rows, cols, stream)
     else:
         assert native.dense(out, x, plan.rows, cols)
     w, w_dtype = _weights(weights, plan)
@@ -663,7 +678,7 @@ def nvfp4_expert_combine(rows, plan, weights=None, out=None, stream=None):
     cols, _ = native.matrix(rows, plan.rows)
     assert native.dense(rows, None, plan.rows, cols)
     if out is None:
-        out = native.empty_rows(rows, plan.tokens, cols)
+        out = native.empty_rows(rows, plan.tokens, cols, stream)
     else:
         assert native.dense(out, rows, plan.tokens, cols)
     w, w_dtype = _weights(weights, plan)
@@ -680,9 +695,9 @@ def nvfp4_expert_combine_bwd(dy, rows, plan, weights, rows_gradient: bool = True
     if drows is not None:
         assert native.dense(drows, rows, plan.rows, cols)
     elif rows_gradient:
-        drows = native.empty_rows(rows, plan.rows, cols)
+        drows = native.empty_rows(rows, plan.rows, cols, stream)
     if dweights is None:
-        dweights = native.empty_rows(weights, plan.tokens, plan.topk)
+        dweights = native.empty_rows(weights, plan.tokens, plan.topk, stream)
     else:
         assert native.dense(dweights, weights, plan.tokens, plan.topk)
     st = native.nvfp4_expert_combine_bwd(dy, dy, plan.tokens, plan.topk, plan.experts, cols, ld, plan.offsets, plan.slot_of, plan.row_of,
@@ -696,7 +711,7 @@ def nvfp4_quantize_fp8_experts(x, plan, weights=None, sorted_rows: bool = False,
     multiplied by weights.  Returns (codes [rows, cols], scales, codes_t [cols, rows], scales_t)."""
     native = _native()
     cols, ld = native.matrix(x, plan.rows if sorted_rows else plan.tokens)
-    out = native.empty_fp8(x, 0, plan.rows, cols, int(row), int(transposed), SF_SWIZZLED)
+    out = native.empty_fp8(x, 0, plan.rows, cols, int(row), int(transposed), SF_SWIZZLED, stream)
     w, w_dtype = _weights(weights, plan)
     st = native.nvfp4_quantize_fp8_experts(x, x, int(not sorted_rows), plan.tokens, plan.topk, plan.experts, cols, ld, plan.offsets,
                                            plan.slot_of, w, w_dtype, *out, stream)
@@ -710,7 +725,7 @@ def nvfp4_gemm_fp8_experts(a_codes, a_sf, b_codes, b_sf, plan, out_dtype=torch.f
     (a, R, K), (E, N, Kb) = native.fp8_operand(a_codes, a_sf), native.fp8_operand(b_codes, b_sf)
     assert K == Kb and a == 1 and R == plan.rows and E == plan.experts
     if out is None:
-        out = _product_rows(R, N, out_dtype, a_codes.device)
+        out = _product_rows(R, N, out_dtype, a_codes, stream)
     assert out.shape == (R, N) and out.stride(1) == 1
     st = native.nvfp4_gemm_fp8_experts(a_codes, a_sf, b_codes, b_sf, plan.tokens, plan.topk, E, plan.counts, plan.offsets, N, K, out, out,
                                           out.stride(0), stream)
@@ -724,7 +739,7 @@ def nvfp4_gemm_fp8_experts_dw(a_codes, a_sf, b_codes, b_sf, plan, out_dtype=torc
     (a, N, R), (b, K, Rb) = native.fp8_operand(a_codes, a_sf), native.fp8_operand(b_codes, b_sf)
     assert a == b == 1 and R == Rb == plan.rows
     if out is None:
-        out = torch.empty((plan.experts, N, K), dtype=out_dtype, device=a_codes.device)
+        out = _empty((plan.experts, N, K), out_dtype, a_codes, stream)
     assert out.shape == (plan.experts, N, K) and out.is_contiguous()
     st = native.nvfp4_gemm_fp8_experts_dw(a_codes, a_sf, b_codes, b_sf, plan.tokens, plan.topk, plan.experts, plan.offsets, N, K, out, out, stream)
     _check(st, "nvfp4_gemm_fp8_experts_dw")
@@ -740,11 +755,11 @@ def nvfp4_experts_fp8_fwd(X, W, plan, sorted_rows: bool = False, out=None, out_d
     X is [rows, K] already).  Y [rows, N] of X's dtype unless told otherwise."""
     native, (E, N, K) = _native(), W.shape
     if out is None:
-        out = torch.empty((plan.rows, N), dtype=out_dtype or X.dtype, device=X.device)
+        out = _empty((plan.rows, N), out_dtype or X.dtype, X, stream)
     assert native.dense(X, W, plan.rows if sorted_rows else plan.tokens, K) and native.dense(W, None, plan.experts, N, K)
     assert native.dense(out, None, plan.rows, N)
     if workspace is None:
-        workspace = _scratch(nvfp4_experts_fp8_workspace_bytes(plan.tokens, plan.topk, E, N, K, FP8_FWD), X.device, None)
+        workspace = _scratch(nvfp4_experts_fp8_workspace_bytes(plan.tokens, plan.topk, E, N, K, FP8_FWD), X, None, stream)
     st = native.nvfp4_experts_fp8_fwd(X, int(not sorted_rows), W, X, plan.tokens, plan.topk, E, N, K, plan.offsets, plan.slot_of, out, out,
                                       workspace, workspace, stream)
     _check(st, "nvfp4_experts_fp8_fwd")
@@ -757,14 +772,14 @@ def nvfp4_experts_fp8_bwd(dY, W, X, plan, weights=None, dy_sorted_rows: bool = F
     nvfp4_expert_combine (dy_sorted_rows: dY is [rows, N] already); X as in nvfp4_experts_fp8_fwd.  Returns (dX, dW)."""
     native, (E, N, K) = _native(), W.shape
     if dX is None:
-        dX = torch.empty((plan.rows, K), dtype=dx_dtype or X.dtype, device=dY.device)
+        dX = _empty((plan.rows, K), dx_dtype or X.dtype, dY, stream)
     if dW is None:
-        dW = torch.empty((E, N, K), dtype=dw_dtype, device=dY.device)
+        dW = _empty((E, N, K), dw_dtype, dY, stream)
     assert native.dense(dY, W, plan.rows if dy_sorted_rows else plan.tokens, N) and native.dense(X, W, plan.rows if sorted_rows else plan.tokens, K)
     assert native.dense(W, None, plan.experts, N, K) and native.dense(dX, None, plan.rows, K) and native.dense(dW, None, E, N, K)
     w, w_dtype = _weights(weights, plan)
     if workspace is None:
-        workspace = _scratch(nvfp4_experts_fp8_workspace_bytes(plan.tokens, plan.topk, E, N, K, FP8_BWD), dY.device, None)
+        workspace = _scratch(nvfp4_experts_fp8_workspace_bytes(plan.tokens, plan.topk, E, N, K, FP8_BWD), dY, None, stream)
     st = native.nvfp4_experts_fp8_bwd(dY, int(not dy_sorted_rows), w, w_dtype, W, X, int(not sorted_rows), dY, plan.tokens, plan.topk, E, N, K,
                                       plan.offsets, plan.slot_of, dX, dX, dW, dW, workspace, workspace, stream)
     _check(st, "nvfp4_experts_fp8_bwd")
@@ -782,7 +797,7 @@ def nvfp4_linear_fwd_static(X, W, gscale_mode=G_AMAX, gx=None, gw=None, rx=None,
     that may overlap on the GPU must be serialised.  Larger layers raise (status 5)."""
     (M, K), N = X.shape, W.shape[0]
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype, device=X.device)
+        out = _empty((M, N), out_dtype, X, stream)
     rx, rw = rx or Rounding(RTN), rw or Rounding(RTN)
     assert X.is_contiguous() and W.is_contiguous() and out.is_contiguous() and X.dtype == W.dtype
     st = _native().nvfp4_linear_fwd_static(X, W, X, M, N, K, gscale_mode, gx, gw, rx, rw, out, out, stream)
@@ -794,7 +809,8 @@ def nvfp4_microbench_mma_peak(stages: int, instr_n: int = 256, device=None, stre
     """Issue-rate measurement of the FP4 tensor-core instruction: returns an int64 tensor [pairs, 3] of
     (cycles, instructions, timed-out flag) per CTA pair."""
     dev = torch.device("cuda", torch.cuda.current_device()) if device is None else device
-    out = torch.zeros((torch.cuda.get_device_properties(dev).multi_processor_count // 2 + 1, 3), dtype=torch.int64, device=dev)
+    with torch.cuda.stream(stream):          # cleared there too
+        out = torch.zeros((torch.cuda.get_device_properties(dev).multi_processor_count // 2 + 1, 3), dtype=torch.int64, device=dev)
     pairs = C.c_int(0)
     _check(lib().nvfp4_microbench_mma_peak(stages, instr_n, _ptr(out), out.numel() * 8, C.byref(pairs), _stream(stream)),
            "nvfp4_microbench_mma_peak")

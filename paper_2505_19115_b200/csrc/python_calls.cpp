@@ -13,16 +13,24 @@
 //
 // The outputs that a caller of the FP8 and expert calls does not give are made here too: torch.empty and a slice from Python take 2.6 and
 // 1.1 us each, which for four of them is more than the launch (quantizing both ways 24 -> 10 us of host time).
+//
+// Memory for a call that is given a stream is allocated on that stream (OnStream below): the allocator hands a block out again in the
+// order of the stream that it was allocated on, so that one of the current stream's could still be written by work queued there
+// earlier, or be given away while the call's kernels use it.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <dlfcn.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
+#include <optional>
 #include <tuple>
 #include <type_traits>
 #include <utility>
@@ -186,6 +194,28 @@ PyObject* wrap(const at::Tensor& t) {
   return o;
 }
 at::Tensor empty(const at::Tensor& like, at::IntArrayRef size, at::ScalarType type) { return at::empty(size, like.options().dtype(type)); }
+
+// While it lives, memory on the device of `like` is allocated on the given stream (None: on the current one).  leave(t): t goes to the
+// caller, who may use it on the stream that is current now, in the order of that stream, and drop it.
+class OnStream {
+ public:
+  OnStream(PyObject* stream, const at::Tensor& like) {
+    if (stream == Py_None || !like.is_cuda()) return;
+    const c10::DeviceIndex device = like.device().index();
+    const c10::cuda::CUDAStream here = c10::cuda::getCurrentCUDAStream(device);
+    const cudaStream_t handle = static_cast<cudaStream_t>(stream_handle(stream));
+    if (handle == here.stream()) return;
+    before_ = here;
+    guard_.emplace(handle ? c10::cuda::getStreamFromExternal(handle, device) : c10::cuda::getDefaultCUDAStream(device));
+  }
+  void leave(const at::Tensor& t) const {
+    if (before_ && t.defined()) c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), *before_);
+  }
+
+ private:
+  std::optional<c10::cuda::CUDAStream> before_;
+  std::optional<c10::cuda::CUDAStreamGuard> guard_;
+};
 const at::Tensor& tensor(PyObject* o) {
   if (!THPVariable_Check(o)) type_error("a tensor", o);
   return THPVariable_Unpack(o);
@@ -232,16 +262,23 @@ int wrap_all(const at::Tensor (&out)[4], PyObject** made) {
   return 4;
 }
 
+// Each of the functions that make outputs takes the stream of the call last, or not at all.
+bool has_arguments(Py_ssize_t n, Py_ssize_t expected) {
+  if (n == expected || n == expected + 1) return true;
+  PyErr_Format(PyExc_TypeError, "expected %zd arguments, and a stream or None", expected);
+  return false;
+}
+PyObject* last(PyObject* const* args, Py_ssize_t n, Py_ssize_t expected) { return n > expected ? args[expected] : Py_None; }
+
 // empty_fp8(like, batch, rows, cols, row, transposed, sf_layout): (codes, scales, codes_t, scales_t), None for what is not wanted.
 PyObject* py_empty_fp8(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 7) {
-    PyErr_SetString(PyExc_TypeError, "expected 7 arguments");
-    return nullptr;
-  }
+  if (!has_arguments(n, 7)) return nullptr;
   return tuple_of([&](PyObject** made) {
     const bool wanted[2] = {number(args[4]) != 0, number(args[5]) != 0};
     at::Tensor out[4];
+    const OnStream on(last(args, n, 7), tensor(args[0]));
     make_fp8(tensor(args[0]), number(args[1]), number(args[2]), number(args[3]), wanted, number(args[6]), out);
+    for (const at::Tensor& t : out) on.leave(t);
     return wrap_all(out, made);
   });
 }
@@ -269,7 +306,9 @@ PyObject* py_quantize_fp8(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const int64_t ld = rows * std::max<int64_t>(batch, 1) == 1 ? (cols + 7) / 8 * 8 : d == 3 ? cols : x.stride(0);
     void* const stream = stream_handle(args[5]);
     at::Tensor out[4];
+    const OnStream on(args[5], x);
     make_fp8(x, batch, rows, cols, wanted, layout, out);
+    for (const at::Tensor& t : out) on.leave(t);
     uint8_t* to[4];
     for (int i = 0; i < 4; ++i) to[i] = out[i].defined() ? static_cast<uint8_t*>(out[i].data_ptr()) : nullptr;
     Py_BEGIN_ALLOW_THREADS
@@ -285,15 +324,14 @@ PyObject* py_quantize_fp8(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 // expert_buffers(like, tokens, topk, experts, rows): (counts, offsets, row_of, slot_of)
 PyObject* py_expert_buffers(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 5) {
-    PyErr_SetString(PyExc_TypeError, "expected 5 arguments");
-    return nullptr;
-  }
+  if (!has_arguments(n, 5)) return nullptr;
   return tuple_of([&](PyObject** made) {
     const at::Tensor& like = tensor(args[0]);
     const int64_t tokens = number(args[1]), topk = number(args[2]), experts = number(args[3]), rows = number(args[4]);
+    const OnStream on(last(args, n, 5), like);
     // one buffer; a tensor of its own for each would cost a microsecond
     const at::Tensor buffer = empty(like, {rows + tokens * topk + 2 * experts + 1}, at::kInt);
+    on.leave(buffer);
     int64_t at = 0;
     auto part = [&](std::initializer_list<int64_t> size, int64_t n) {
       at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(buffer.storage()), buffer.key_set(), buffer.dtype());
@@ -348,13 +386,35 @@ PyObject* py_dense(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 // empty_rows(like, rows, cols): [rows, cols] of like's dtype
 PyObject* py_empty_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 3) {
-    PyErr_SetString(PyExc_TypeError, "expected 3 arguments");
+  if (!has_arguments(n, 3)) return nullptr;
+  try {
+    const at::Tensor& like = tensor(args[0]);
+    const OnStream on(last(args, n, 3), like);
+    const at::Tensor t = empty(like, {number(args[1]), number(args[2])}, like.scalar_type());
+    on.leave(t);
+    return wrap(t);
+  } catch (const PythonError&) {
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+  }
+  return nullptr;
+}
+// empty_on(stream, like, dtype, leaves, size...): on like's device; leaves: it goes to the caller of the call that uses it
+PyObject* py_empty_on(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  constexpr Py_ssize_t kFixed = 4, kMostDims = 4;
+  if (n <= kFixed || n > kFixed + kMostDims || !THPDtype_Check(args[2])) {
+    PyErr_SetString(PyExc_TypeError, "expected a stream or None, a tensor, a dtype, a number and sizes");
     return nullptr;
   }
   try {
-    const at::Tensor& like = tensor(args[0]);
-    return wrap(empty(like, {number(args[1]), number(args[2])}, like.scalar_type()));
+    int64_t size[kMostDims];
+    for (Py_ssize_t i = kFixed; i < n; ++i) size[i - kFixed] = number(args[i]);
+    const bool leaves = number(args[3]) != 0;
+    const at::Tensor& like = tensor(args[1]);
+    const OnStream on(args[0], like);
+    const at::Tensor t = empty(like, at::IntArrayRef(size, n - kFixed), reinterpret_cast<THPDtype*>(args[2])->scalar_type);
+    if (leaves) on.leave(t);
+    return wrap(t);
   } catch (const PythonError&) {
   } catch (const std::exception& e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
@@ -420,7 +480,7 @@ PyObject* py_bind(PyObject*, PyObject* args) {
 
 #define NVFP4_METHOD(name, ...) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr},
 #define NVFP4_HELPER(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {{"bind", py_bind, METH_VARARGS, nullptr}, NVFP4_HELPER(empty_fp8), NVFP4_HELPER(expert_buffers), NVFP4_HELPER(empty_rows), NVFP4_HELPER(fp8_operand),
+PyMethodDef methods[] = {{"bind", py_bind, METH_VARARGS, nullptr}, NVFP4_HELPER(empty_fp8), NVFP4_HELPER(expert_buffers), NVFP4_HELPER(empty_rows), NVFP4_HELPER(empty_on), NVFP4_HELPER(fp8_operand),
                          NVFP4_HELPER(quantize_fp8), NVFP4_HELPER(matrix), NVFP4_HELPER(dense),
                          NVFP4_CALLS(NVFP4_METHOD) NVFP4_CALLS_HERE(NVFP4_METHOD){nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
