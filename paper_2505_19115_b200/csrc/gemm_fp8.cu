@@ -93,11 +93,8 @@ __device__ __forceinline__ void tile_coords(int tile, int tiles_m, int tiles_n, 
   tm = panel * kPanel + in_panel - tn * height;
 }
 
-// The tensor core adds to its accumulator with truncation, so that an error grows with the number of additions: on normal values
-// 7e-7 of the result at a contraction of 11008, over 1e-6 at 16384 (a sum in fp32 rounded at every step: 2e-7).  Contractions longer than
-// kMostBlocks blocks are summed in equal parts, which the epilogue adds up in registers (LONG: a kernel of their own, since the others lose
-// 2 % by the choice).  A part costs a turn-round of the accumulator.
-constexpr int kMostBlocks = 96;
+// Contractions longer than kMostBlocks blocks are summed in equal parts, which the epilogue adds up in registers (LONG: a kernel of
+// their own, since the others lose 2 % by the choice).  A part costs a turn-round of the accumulator.
 template <bool LONG>
 __device__ __forceinline__ int part_blocks(int blocks, int sub) {
   if (!LONG || blocks <= kMostBlocks) return blocks;

@@ -14,6 +14,8 @@
 // One product: with few tiles of B a cluster of 2, 4 or 8 blocks shares one along the contraction axis; each then sums a share of
 // the tokens over all blocks' accumulators, which they write into one another's shared memory, in the order of the blocks.
 // Segments (experts): the blocks go over the tiles of all segments with rows, one tile at a time.
+// A block whose contraction is longer than kMostBlocks stages sums it in equal parts: the epilogue adds up the accumulators in columns
+// of tensor memory of their own, so that it needs no more registers and a contraction of one part runs as before.
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -35,13 +37,14 @@ constexpr int kSfBytes = 2 * 512;                   // a scale tile of B's rows 
 constexpr int kMaxStages = 12;
 constexpr int kSfSlots = 4;                         // scale tiles of four stages each
 constexpr int kRingBytes = 200 * 1024;
-constexpr uint32_t kTmemCols = 256;
+constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kSfCol = 128;                    // accumulators: columns 0-127; then 8 columns of scales per slot
+constexpr uint32_t kSumCol = 256;                   // sums of the parts so far, 128 columns
 constexpr int kTableBytes = 3 * (int)(kMaxExperts + 1) * 4 + 4;
 constexpr int kBarrierBytes = 512;
 constexpr int kSmemBytes = 1024 /*align*/ + kRingBytes + kSfSlots * kSfBytes + kBarrierBytes + kTableBytes;
 static_assert(kSmemBytes <= 232448, "shared memory overflow");
-static_assert(kSfCol + 8 * kSfSlots <= kTmemCols, "tensor memory overflow");
+static_assert(kSfCol + 8 * kSfSlots <= kSumCol && kSumCol + kMaxTokens <= kTmemCols, "tensor memory overflow");
 static_assert(8 * (2 * kMaxStages + 3 * kSfSlots + 4) + 8 <= kBarrierBytes, "barrier area overflow");
 static_assert(kMaxTokens * 128 * 4 <= kRingBytes, "the ring holds a share of all blocks' accumulators");
 
@@ -100,6 +103,20 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8])
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
+// 32 columns of an accumulator, plus those of the parts before it where there are any.
+__device__ __forceinline__ void load_sums(uint32_t acc, uint32_t sums, bool more, uint32_t (&r)[32]) {
+  tmem_ld32(acc, r);
+  tmem_ld_wait();
+  tmem_ld_pin(r);
+  if (more) {
+    uint32_t s[32];
+    tmem_ld32(sums, s);
+    tmem_ld_wait();
+    tmem_ld_pin(s);
+#pragma unroll
+    for (int c = 0; c < 32; ++c) r[c] = __float_as_uint(__uint_as_float(r[c]) + __uint_as_float(s[c]));
+  }
+}
 __device__ __forceinline__ void store_as(__nv_bfloat16* d, float v) { *d = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void store_as(float* d, float v) { *d = v; }
 // Up to 32 values of a column of D, one below the other.
@@ -138,6 +155,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp8_few_kernel(const __grid_
   const int rank = p.split > 1 ? (int)cluster_ctarank() : 0;
   const int first_item = blockIdx.x / p.split, items_step = gridDim.x / p.split;
   const int ks0 = p.k_stages * rank / p.split, ks1 = p.k_stages * (rank + 1) / p.split;
+  // an accumulator takes a part of the block's contraction at a time
+  const int at_least = (ks1 - ks0 + kMostBlocks - 1) / kMostBlocks, part = (ks1 - ks0 + at_least - 1) / at_least, parts = (ks1 - ks0 + part - 1) / part;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
@@ -248,9 +267,18 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp8_few_kernel(const __grid_
       if (first) { follow(); first = false; }
       ok = mbar_wait_issuer(tempty_bar(acc), acc_ph ^ 1u, abort_flag, 0x62);
       if (!ok) break;
-      const uint32_t d_tmem = tmem_base + acc * 64;
+      uint32_t d_tmem = tmem_base + acc * 64;
       const uint32_t idesc0 = instr_desc_mxf8(128, (t.rows + 15) & ~15, 0);
+      int begin = ks0;                              // of the part
       for (int ks = ks0; ks < ks1; ++ks) {
+        if (ks == begin + part) {
+          begin = ks;
+          if (issuer) tc_commit(tfull_bar(acc));
+          if (++acc == acc_stages) { acc = 0; acc_ph ^= 1u; }
+          ok = mbar_wait_issuer(tempty_bar(acc), acc_ph ^ 1u, abort_flag, 0x62);
+          if (!ok) break;
+          d_tmem = tmem_base + acc * 64;
+        }
         if (ks == ks0 || !(ks & 3)) ok = mbar_wait_issuer(sfr_bar(q), q_ph, abort_flag, 0x65);
         ok = ok && mbar_wait_issuer(full_bar(s), ph, abort_flag, 0x63);
         if (!ok) break;
@@ -261,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp8_few_kernel(const __grid_
         const uint64_t wdesc = operand_desc(st), xdesc = operand_desc(st + kWBytes);
         const int n = min(4, p.k_mmas - ks * 4);
         if (issuer) {
-          for (int j = 0; j < n; ++j) tc_mma_mxf8(d_tmem, wdesc + 2u * j, xdesc + 2u * j, idesc, sfw_t, sfx_t, (ks > ks0 || j) ? 1u : 0u);
+          for (int j = 0; j < n; ++j) tc_mma_mxf8(d_tmem, wdesc + 2u * j, xdesc + 2u * j, idesc, sfw_t, sfx_t, (ks > begin || j) ? 1u : 0u);
           tc_commit(empty_bar(s));
           if ((ks & 3) == 3 || ks == ks1 - 1) tc_commit(sfe_bar(q));
         }
@@ -303,20 +331,36 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp8_few_kernel(const __grid_
     const int quarter = warp & 3;
     int acc = 0;
     uint32_t acc_ph = 0;
-    bool first = true;
+    bool ok = true, first = true;
     Item t;
-    for (int i = first_item; item_at(p, tab, i, t); i += items_step) {
+    for (int i = first_item; ok && item_at(p, tab, i, t); i += items_step) {
       if (first) { follow(); first = false; }
-      if (!mbar_wait_warp_spin(tfull_bar(acc), acc_ph, abort_flag, 0x64)) break;
-      if (p.split > 1) break;                       // one item: the sums over the cluster follow below
+      const uint32_t sum_row = tmem_base + kSumCol + ((uint32_t)(quarter * 32) << 16);
+      for (int n = 1; n < parts; ++n) {             // all parts but the last go into the sums
+        ok = mbar_wait_warp_spin(tfull_bar(acc), acc_ph, abort_flag, 0x64);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t t_row = tmem_base + acc * 64 + ((uint32_t)(quarter * 32) << 16);
+        for (int c0 = 0; c0 < t.rows; c0 += 32) {
+          uint32_t r[32];
+          load_sums(t_row + c0, sum_row + c0, n > 1, r);
+          tmem_st16(sum_row + c0, *reinterpret_cast<const uint32_t(*)[16]>(r));
+          tmem_st16(sum_row + c0 + 16, *reinterpret_cast<const uint32_t(*)[16]>(r + 16));
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(tempty_bar(acc));
+        if (++acc == acc_stages) { acc = 0; acc_ph ^= 1u; }
+      }
+      ok = ok && mbar_wait_warp_spin(tfull_bar(acc), acc_ph, abort_flag, 0x64);
+      if (!ok || p.split > 1) break;                // one item: the sums over the cluster follow below
       tc_fence_after();
       const uint32_t t_row = tmem_base + acc * 64 + ((uint32_t)(quarter * 32) << 16);
       const int n = t.n0 + quarter * 32 + lane;
       for (int c0 = 0; c0 < t.rows; c0 += 32) {
         uint32_t r[32];
-        tmem_ld32(t_row + c0, r);
-        tmem_ld_wait();
-        tmem_ld_pin(r);
+        load_sums(t_row + c0, sum_row + c0, parts > 1, r);
         if (c0 + 32 >= t.rows) {
           tc_fence_before();
           __syncwarp();
@@ -342,13 +386,12 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp8_few_kernel(const __grid_
     // (in steps of eight, so that a lane's eight stores go to one block: a block and an address for every column cost 75 cycles each)
     const int share = ((p.M + 7) / 8 + p.split - 1) / p.split * 8, tile = first_item;
     if (warp >= 8) {
-      const uint32_t t_row = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
+      const uint32_t quarter_row = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
+      const uint32_t t_row = quarter_row + (parts - 1) % acc_stages * 64, sum_row = quarter_row + kSumCol;
       const uint32_t mine = smem_base + (uint32_t)(rank * share * 128 + (warp & 3) * 32 + lane) * 4u;
       for (int c0 = 0; c0 < p.M; c0 += 32) {
         uint32_t r[32];
-        tmem_ld32(t_row + c0, r);
-        tmem_ld_wait();
-        tmem_ld_pin(r);
+        load_sums(t_row + c0, sum_row + c0, parts > 1, r);
 #pragma unroll
         for (int c = 0; c < 32; c += 8) {
           if (c0 + c >= p.M) break;
