@@ -422,8 +422,9 @@ PyObject* py_empty_on(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return nullptr;
 }
 
-// fp8_operand(codes, scales): (matrices, Rq, Kq) of codes as the quantizer leaves them, with swizzled scales.  Other layouts and buffers
-// that are too small are refused: the products would read behind them.
+// fp8_operand(codes, scales): (matrices, Rq, Kq) of codes as the quantizer leaves them, with swizzled scales: flat, or in rows of whole
+// tiles.  Buffers that are too small are refused, since the products would read behind them, and so are linear scales, whose rows are a
+// byte for each block: they may have just as many bytes.
 PyObject* py_fp8_operand(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (n != 2) {
     PyErr_SetString(PyExc_TypeError, "expected 2 arguments");
@@ -441,9 +442,10 @@ PyObject* py_fp8_operand(PyObject*, PyObject* const* args, Py_ssize_t n) {
       PyErr_SetString(PyExc_ValueError, "rows of FP8 codes take a multiple of 16 bytes and lie one behind the other");
       return nullptr;
     }
-    const int64_t tiles = b * ((rq + 127) / 128) * (((kq + 127) / 128 + 3) / 4);
-    if (scales.element_size() != 1 || !scales.is_contiguous() || scales.numel() < tiles * 512) {
-      PyErr_SetString(PyExc_ValueError, "FP8 codes come with a flat buffer of swizzled scales");
+    const int64_t nb = (kq + 127) / 128, tiles = b * ((rq + 127) / 128) * ((nb + 3) / 4), sd = scales.dim();
+    const bool in_tiles = sd == 1 || (sd > 1 && scales.size(sd - 1) % 512 == 0 && scales.size(sd - 1) != nb);
+    if (scales.element_size() != 1 || !scales.is_contiguous() || !in_tiles || scales.numel() < tiles * 512) {
+      PyErr_SetString(PyExc_ValueError, "FP8 codes come with swizzled scales, in whole tiles of 512 bytes");
       return nullptr;
     }
     return Py_BuildValue("(LLL)", (long long)b, (long long)rq, (long long)kq);
