@@ -541,6 +541,12 @@ def nvfp4_linear_bwd_bf16(dY, W, X, dx_dtype=torch.float32, dw_dtype=torch.float
 FP8_FWD, FP8_BWD = 0, 1
 
 
+def _require(ok, call):
+    """Raised, not asserted: a kernel would read or write behind a tensor that is too small."""
+    if not ok:
+        raise ValueError(f"{call}: a tensor is not of the size, the dtype or the layout that the call takes")
+
+
 def nvfp4_codes_bytes_fp8(Rq: int, Kq: int) -> int:
     return int(lib().nvfp4_codes_bytes_fp8(Rq, Kq))
 
@@ -570,10 +576,10 @@ def nvfp4_gemm_fp8(a_codes, a_sf, b_codes, b_sf, out_dtype=torch.float32, out=No
     """D[M,N] = A[M,K] . B[N,K]^T on FP8 codes with swizzled scales."""
     native = _native()
     (a, M, K), (b, N, Kb) = native.fp8_operand(a_codes, a_sf), native.fp8_operand(b_codes, b_sf)
-    assert K == Kb and a == b == 1
+    _require(K == Kb and a == b == 1, "nvfp4_gemm_fp8")
     if out is None:
         out = _product_rows(M, N, out_dtype, a_codes, stream)
-    assert out.shape == (M, N) and out.stride(1) == 1
+    _require(out.shape == (M, N) and out.stride(1) == 1, "nvfp4_gemm_fp8")
     st = native.nvfp4_gemm_fp8(a_codes, a_sf, b_codes, b_sf, M, N, K, out, out, out.stride(0), stream)
     _check(st, "nvfp4_gemm_fp8")
     return out
@@ -589,7 +595,7 @@ def nvfp4_linear_fp8_fwd(X, W, out=None, out_dtype=torch.float32, workspace=None
     if out is None:
         out = _empty((M, N), out_dtype, X, stream)
     native = _native()
-    assert native.dense(X, None, M, K) and native.dense(W, X, N, K) and native.dense(out, None, M, N)
+    _require(native.dense(X, None, M, K) and native.dense(W, X, N, K) and native.dense(out, None, M, N), "nvfp4_linear_fp8_fwd")
     if workspace is None:
         workspace = _scratch(nvfp4_linear_fp8_workspace_bytes(M, N, K, FP8_FWD), X, None, stream)
     st = native.nvfp4_linear_fp8_fwd(X, W, X, M, N, K, out, out, workspace, workspace, stream)
@@ -605,8 +611,8 @@ def nvfp4_linear_fp8_bwd(dY, W, X, dX=None, dW=None, dx_dtype=torch.float32, dw_
     if dW is None:
         dW = _empty((N, K), dw_dtype, dY, stream)
     native = _native()
-    assert native.dense(dY, None, M, N) and native.dense(W, dY, N, K) and native.dense(X, dY, M, K)
-    assert native.dense(dX, None, M, K) and native.dense(dW, None, N, K)
+    _require(native.dense(dY, None, M, N) and native.dense(W, dY, N, K) and native.dense(X, dY, M, K) and
+             native.dense(dX, None, M, K) and native.dense(dW, None, N, K), "nvfp4_linear_fp8_bwd")
     if workspace is None:
         workspace = _scratch(nvfp4_linear_fp8_workspace_bytes(M, N, K, FP8_BWD), dY, None, stream)
     st = native.nvfp4_linear_fp8_bwd(dY, W, X, dY, M, N, K, dX, dX, dW, dW, workspace, workspace, stream)
@@ -639,21 +645,21 @@ def nvfp4_expert_sort(expert_of, experts: int, plan: ExpertPlan = None, stream=N
     if not wide and expert_of.dtype is not torch.int32:
         raise TypeError(f"unsupported dtype {expert_of.dtype}")
     tokens, topk = expert_of.shape
-    assert _native().dense(expert_of, None, tokens, topk)
+    _require(_native().dense(expert_of, None, tokens, topk), "nvfp4_expert_sort")
     if plan is None:
         plan = ExpertPlan(tokens, topk, experts, expert_of, stream)
     else:
-        assert (plan.tokens, plan.topk, plan.experts) == (tokens, topk, experts)
+        _require((plan.tokens, plan.topk, plan.experts) == (tokens, topk, experts), "nvfp4_expert_sort")
     st = _native().nvfp4_expert_sort(expert_of, int(wide), tokens, topk, experts, plan.counts, plan.offsets, plan.row_of, plan.slot_of, stream)
     _check(st, "nvfp4_expert_sort")
     return plan
 
 
-def _weights(weights, plan):
+def _weights(weights, plan, call):
     """(tensor or None, its dtype for the call)."""
     if weights is None:
         return None, BF16
-    assert _native().dense(weights, None, plan.tokens, plan.topk)
+    _require(_native().dense(weights, None, plan.tokens, plan.topk), call)
     return weights, weights
 
 
@@ -664,8 +670,8 @@ def nvfp4_expert_gather(x, plan, weights=None, out=None, stream=None):
     if out is None:
         out = native.empty_rows(x, plan.rows, cols, stream)
     else:
-        assert native.dense(out, x, plan.rows, cols)
-    w, w_dtype = _weights(weights, plan)
+        _require(native.dense(out, x, plan.rows, cols), "nvfp4_expert_gather")
+    w, w_dtype = _weights(weights, plan, "nvfp4_expert_gather")
     st = native.nvfp4_expert_gather(x, x, plan.tokens, plan.topk, plan.experts, cols, ld, plan.offsets, plan.slot_of, plan.row_of,
                                     w, w_dtype, out, stream)
     _check(st, "nvfp4_expert_gather")
@@ -676,12 +682,12 @@ def nvfp4_expert_combine(rows, plan, weights=None, out=None, stream=None):
     """y[t] = sum_j (weights[t,j] *) rows[row of (t,j)]; without weights the gradient of nvfp4_expert_gather."""
     native = _native()
     cols, _ = native.matrix(rows, plan.rows)
-    assert native.dense(rows, None, plan.rows, cols)
+    _require(native.dense(rows, None, plan.rows, cols), "nvfp4_expert_combine")
     if out is None:
         out = native.empty_rows(rows, plan.tokens, cols, stream)
     else:
-        assert native.dense(out, rows, plan.tokens, cols)
-    w, w_dtype = _weights(weights, plan)
+        _require(native.dense(out, rows, plan.tokens, cols), "nvfp4_expert_combine")
+    w, w_dtype = _weights(weights, plan, "nvfp4_expert_combine")
     st = native.nvfp4_expert_combine(rows, rows, plan.tokens, plan.topk, plan.experts, cols, plan.row_of, w, w_dtype, out, stream)
     _check(st, "nvfp4_expert_combine")
     return out
@@ -691,15 +697,15 @@ def nvfp4_expert_combine_bwd(dy, rows, plan, weights, rows_gradient: bool = True
     """Gradient of nvfp4_expert_combine by its rows and its weights: (drows, or None where it is not wanted; dweights)."""
     native = _native()
     cols, ld = native.matrix(dy, plan.tokens)
-    assert native.dense(rows, dy, plan.rows, cols) and native.dense(weights, None, plan.tokens, plan.topk)
+    _require(native.dense(rows, dy, plan.rows, cols) and native.dense(weights, None, plan.tokens, plan.topk), "nvfp4_expert_combine_bwd")
     if drows is not None:
-        assert native.dense(drows, rows, plan.rows, cols)
+        _require(native.dense(drows, rows, plan.rows, cols), "nvfp4_expert_combine_bwd")
     elif rows_gradient:
         drows = native.empty_rows(rows, plan.rows, cols, stream)
     if dweights is None:
         dweights = native.empty_rows(weights, plan.tokens, plan.topk, stream)
     else:
-        assert native.dense(dweights, weights, plan.tokens, plan.topk)
+        _require(native.dense(dweights, weights, plan.tokens, plan.topk), "nvfp4_expert_combine_bwd")
     st = native.nvfp4_expert_combine_bwd(dy, dy, plan.tokens, plan.topk, plan.experts, cols, ld, plan.offsets, plan.slot_of, plan.row_of,
                                          rows, weights, weights, drows, dweights, stream)
     _check(st, "nvfp4_expert_combine_bwd")
@@ -712,7 +718,7 @@ def nvfp4_quantize_fp8_experts(x, plan, weights=None, sorted_rows: bool = False,
     native = _native()
     cols, ld = native.matrix(x, plan.rows if sorted_rows else plan.tokens)
     out = native.empty_fp8(x, 0, plan.rows, cols, int(row), int(transposed), SF_SWIZZLED, stream)
-    w, w_dtype = _weights(weights, plan)
+    w, w_dtype = _weights(weights, plan, "nvfp4_quantize_fp8_experts")
     st = native.nvfp4_quantize_fp8_experts(x, x, int(not sorted_rows), plan.tokens, plan.topk, plan.experts, cols, ld, plan.offsets,
                                            plan.slot_of, w, w_dtype, *out, stream)
     _check(st, "nvfp4_quantize_fp8_experts")
@@ -723,10 +729,10 @@ def nvfp4_gemm_fp8_experts(a_codes, a_sf, b_codes, b_sf, plan, out_dtype=torch.f
     """D[r] = A[r] . B[e]^T for the rows r of expert e; A [rows, K], B [experts, N, K]."""
     native = _native()
     (a, R, K), (E, N, Kb) = native.fp8_operand(a_codes, a_sf), native.fp8_operand(b_codes, b_sf)
-    assert K == Kb and a == 1 and R == plan.rows and E == plan.experts
+    _require(K == Kb and a == 1 and R == plan.rows and E == plan.experts, "nvfp4_gemm_fp8_experts")
     if out is None:
         out = _product_rows(R, N, out_dtype, a_codes, stream)
-    assert out.shape == (R, N) and out.stride(1) == 1
+    _require(out.shape == (R, N) and out.stride(1) == 1, "nvfp4_gemm_fp8_experts")
     st = native.nvfp4_gemm_fp8_experts(a_codes, a_sf, b_codes, b_sf, plan.tokens, plan.topk, E, plan.counts, plan.offsets, N, K, out, out,
                                           out.stride(0), stream)
     _check(st, "nvfp4_gemm_fp8_experts")
@@ -737,10 +743,10 @@ def nvfp4_gemm_fp8_experts_dw(a_codes, a_sf, b_codes, b_sf, plan, out_dtype=torc
     """D[e] = A[:, rows of e] . B[:, rows of e]^T; A [N, rows], B [K, rows] (transposed outputs of nvfp4_quantize_fp8_experts)."""
     native = _native()
     (a, N, R), (b, K, Rb) = native.fp8_operand(a_codes, a_sf), native.fp8_operand(b_codes, b_sf)
-    assert a == b == 1 and R == Rb == plan.rows
+    _require(a == b == 1 and R == Rb == plan.rows, "nvfp4_gemm_fp8_experts_dw")
     if out is None:
         out = _empty((plan.experts, N, K), out_dtype, a_codes, stream)
-    assert out.shape == (plan.experts, N, K) and out.is_contiguous()
+    _require(out.shape == (plan.experts, N, K) and out.is_contiguous(), "nvfp4_gemm_fp8_experts_dw")
     st = native.nvfp4_gemm_fp8_experts_dw(a_codes, a_sf, b_codes, b_sf, plan.tokens, plan.topk, plan.experts, plan.offsets, N, K, out, out, stream)
     _check(st, "nvfp4_gemm_fp8_experts_dw")
     return out
@@ -756,8 +762,8 @@ def nvfp4_experts_fp8_fwd(X, W, plan, sorted_rows: bool = False, out=None, out_d
     native, (E, N, K) = _native(), W.shape
     if out is None:
         out = _empty((plan.rows, N), out_dtype or X.dtype, X, stream)
-    assert native.dense(X, W, plan.rows if sorted_rows else plan.tokens, K) and native.dense(W, None, plan.experts, N, K)
-    assert native.dense(out, None, plan.rows, N)
+    _require(native.dense(X, W, plan.rows if sorted_rows else plan.tokens, K) and native.dense(W, None, plan.experts, N, K) and
+             native.dense(out, None, plan.rows, N), "nvfp4_experts_fp8_fwd")
     if workspace is None:
         workspace = _scratch(nvfp4_experts_fp8_workspace_bytes(plan.tokens, plan.topk, E, N, K, FP8_FWD), X, None, stream)
     st = native.nvfp4_experts_fp8_fwd(X, int(not sorted_rows), W, X, plan.tokens, plan.topk, E, N, K, plan.offsets, plan.slot_of, out, out,
@@ -775,9 +781,9 @@ def nvfp4_experts_fp8_bwd(dY, W, X, plan, weights=None, dy_sorted_rows: bool = F
         dX = _empty((plan.rows, K), dx_dtype or X.dtype, dY, stream)
     if dW is None:
         dW = _empty((E, N, K), dw_dtype, dY, stream)
-    assert native.dense(dY, W, plan.rows if dy_sorted_rows else plan.tokens, N) and native.dense(X, W, plan.rows if sorted_rows else plan.tokens, K)
-    assert native.dense(W, None, plan.experts, N, K) and native.dense(dX, None, plan.rows, K) and native.dense(dW, None, E, N, K)
-    w, w_dtype = _weights(weights, plan)
+    _require(native.dense(dY, W, plan.rows if dy_sorted_rows else plan.tokens, N) and native.dense(X, W, plan.rows if sorted_rows else plan.tokens, K) and
+             native.dense(W, None, plan.experts, N, K) and native.dense(dX, None, plan.rows, K) and native.dense(dW, None, E, N, K), "nvfp4_experts_fp8_bwd")
+    w, w_dtype = _weights(weights, plan, "nvfp4_experts_fp8_bwd")
     if workspace is None:
         workspace = _scratch(nvfp4_experts_fp8_workspace_bytes(plan.tokens, plan.topk, E, N, K, FP8_BWD), dY, None, stream)
     st = native.nvfp4_experts_fp8_bwd(dY, int(not dy_sorted_rows), w, w_dtype, W, X, int(not sorted_rows), dY, plan.tokens, plan.topk, E, N, K,
