@@ -15,7 +15,8 @@
 // the tokens over all blocks' accumulators, which they write into one another's shared memory, in the order of the blocks.
 // Segments (experts): the blocks go over the tiles of all segments with rows, one tile at a time.
 // A block whose contraction is longer than kMostBlocks stages sums it in equal parts: the epilogue adds up the accumulators in columns
-// of tensor memory of their own, so that it needs no more registers and a contraction of one part runs as before.
+// of tensor memory of their own, which takes no more registers.  us, one accumulator for all of it / in parts: 1 x 9600 x 28672 66.6 / 68.8,
+// 128 rows 71.8 / 75.6, 64 x 8192 x 28672 (two parts) 43.1 / 43.5.
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -37,14 +38,15 @@ constexpr int kSfBytes = 2 * 512;                   // a scale tile of B's rows 
 constexpr int kMaxStages = 12;
 constexpr int kSfSlots = 4;                         // scale tiles of four stages each
 constexpr int kRingBytes = 200 * 1024;
-constexpr uint32_t kTmemCols = 512;
+template <bool LONG>
+constexpr uint32_t kTmemCols = LONG ? 512 : 256;
 constexpr uint32_t kSfCol = 128;                    // accumulators: columns 0-127; then 8 columns of scales per slot
-constexpr uint32_t kSumCol = 256;                   // sums of the parts so far, 128 columns
+constexpr uint32_t kSumCol = 256;                   // LONG: sums of the parts so far, 128 columns
 constexpr int kTableBytes = 3 * (int)(kMaxExperts + 1) * 4 + 4;
 constexpr int kBarrierBytes = 512;
 constexpr int kSmemBytes = 1024 /*align*/ + kRingBytes + kSfSlots * kSfBytes + kBarrierBytes + kTableBytes;
 static_assert(kSmemBytes <= 232448, "shared memory overflow");
-static_assert(kSfCol + 8 * kSfSlots <= kSumCol && kSumCol + kMaxTokens <= kTmemCols, "tensor memory overflow");
+static_assert(kSfCol + 8 * kSfSlots <= kTmemCols<false> && kTmemCols<false> <= kSumCol && kSumCol + kMaxTokens <= kTmemCols<true>, "tensor memory overflow");
 static_assert(8 * (2 * kMaxStages + 3 * kSfSlots + 4) + 8 <= kBarrierBytes, "barrier area overflow");
 static_assert(kMaxTokens * 128 * 4 <= kRingBytes, "the ring holds a share of all blocks' accumulators");
 
@@ -104,11 +106,12 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8])
                ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
 // 32 columns of an accumulator, plus those of the parts before it where there are any.
+template <bool LONG>
 __device__ __forceinline__ void load_sums(uint32_t acc, uint32_t sums, bool more, uint32_t (&r)[32]) {
   tmem_ld32(acc, r);
   tmem_ld_wait();
   tmem_ld_pin(r);
-  if (more) {
+  if (LONG && more) {
     uint32_t s[32];
     tmem_ld32(sums, s);
     tmem_ld_wait();
@@ -129,6 +132,8 @@ __device__ __forceinline__ void store_column(D* d, int64_t ldd, const uint32_t (
   }
 }
 
+// LONG: a block's contraction may be longer than kMostBlocks.  The choice takes 2-3 % of the others' time (1 x 11008 x 4096 13.3 -> 13.6 us).
+template <bool LONG>
 __global__ void __launch_bounds__(kThreads, 1) gemm_fp8_few_kernel(const __grid_constant__ Params p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -156,7 +161,12 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp8_few_kernel(const __grid_
   const int first_item = blockIdx.x / p.split, items_step = gridDim.x / p.split;
   const int ks0 = p.k_stages * rank / p.split, ks1 = p.k_stages * (rank + 1) / p.split;
   // an accumulator takes a part of the block's contraction at a time
-  const int at_least = (ks1 - ks0 + kMostBlocks - 1) / kMostBlocks, part = (ks1 - ks0 + at_least - 1) / at_least, parts = (ks1 - ks0 + part - 1) / part;
+  int part = ks1 - ks0, parts = 1;
+  if constexpr (LONG) {
+    parts = (part + kMostBlocks - 1) / kMostBlocks;
+    part = (part + parts - 1) / parts;
+    parts = (ks1 - ks0 + part - 1) / part;          // fewer where there are very many
+  }
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
@@ -167,7 +177,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp8_few_kernel(const __grid_
     fence_async_smem();
     prefetch_map(&p.w); prefetch_map(&p.x); prefetch_map(&p.sfw); prefetch_map(&p.sfx);
   }
-  if (warp == 1) tmem_alloc(smem_u32((const void*)tmem_slot), kTmemCols);
+  if (warp == 1) tmem_alloc(smem_u32((const void*)tmem_slot), kTmemCols<LONG>);
   if (warp == 2 && p.offsets) {
     // the segments' table: a running sum of the items of 32 segments at a time; what is no plan is cut to the rows that there are
     if (!p.late) grid_dependency_wait();
@@ -271,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp8_few_kernel(const __grid_
       const uint32_t idesc0 = instr_desc_mxf8(128, (t.rows + 15) & ~15, 0);
       int begin = ks0;                              // of the part
       for (int ks = ks0; ks < ks1; ++ks) {
-        if (ks == begin + part) {
+        if (LONG && ks == begin + part) {
           begin = ks;
           if (issuer) tc_commit(tfull_bar(acc));
           if (++acc == acc_stages) { acc = 0; acc_ph ^= 1u; }
@@ -336,14 +346,14 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp8_few_kernel(const __grid_
     for (int i = first_item; ok && item_at(p, tab, i, t); i += items_step) {
       if (first) { follow(); first = false; }
       const uint32_t sum_row = tmem_base + kSumCol + ((uint32_t)(quarter * 32) << 16);
-      for (int n = 1; n < parts; ++n) {             // all parts but the last go into the sums
+      for (int n = 1; LONG && n < parts; ++n) {     // all parts but the last go into the sums
         ok = mbar_wait_warp_spin(tfull_bar(acc), acc_ph, abort_flag, 0x64);
         if (!ok) break;
         tc_fence_after();
         const uint32_t t_row = tmem_base + acc * 64 + ((uint32_t)(quarter * 32) << 16);
         for (int c0 = 0; c0 < t.rows; c0 += 32) {
           uint32_t r[32];
-          load_sums(t_row + c0, sum_row + c0, n > 1, r);
+          load_sums<LONG>(t_row + c0, sum_row + c0, n > 1, r);
           tmem_st16(sum_row + c0, *reinterpret_cast<const uint32_t(*)[16]>(r));
           tmem_st16(sum_row + c0 + 16, *reinterpret_cast<const uint32_t(*)[16]>(r + 16));
         }
@@ -360,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp8_few_kernel(const __grid_
       const int n = t.n0 + quarter * 32 + lane;
       for (int c0 = 0; c0 < t.rows; c0 += 32) {
         uint32_t r[32];
-        load_sums(t_row + c0, sum_row + c0, parts > 1, r);
+        load_sums<LONG>(t_row + c0, sum_row + c0, parts > 1, r);
         if (c0 + 32 >= t.rows) {
           tc_fence_before();
           __syncwarp();
@@ -387,11 +397,11 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp8_few_kernel(const __grid_
     const int share = ((p.M + 7) / 8 + p.split - 1) / p.split * 8, tile = first_item;
     if (warp >= 8) {
       const uint32_t quarter_row = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
-      const uint32_t t_row = quarter_row + (parts - 1) % acc_stages * 64, sum_row = quarter_row + kSumCol;
+      const uint32_t t_row = quarter_row + (LONG ? (parts - 1) % acc_stages * 64 : 0), sum_row = quarter_row + kSumCol;
       const uint32_t mine = smem_base + (uint32_t)(rank * share * 128 + (warp & 3) * 32 + lane) * 4u;
       for (int c0 = 0; c0 < p.M; c0 += 32) {
         uint32_t r[32];
-        load_sums(t_row + c0, sum_row + c0, parts > 1, r);
+        load_sums<LONG>(t_row + c0, sum_row + c0, parts > 1, r);
 #pragma unroll
         for (int c = 0; c < 32; c += 8) {
           if (c0 + c >= p.M) break;
@@ -426,7 +436,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp8_few_kernel(const __grid_
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem_base, kTmemCols);
+    tmem_dealloc(tmem_base, kTmemCols<LONG>);
   }
   grid_dependency_wait();                           // a block without an item has not waited: "finished" keeps meaning "and all before"
 }
@@ -444,6 +454,21 @@ bool byte_map(CUtensorMap* map, const uint8_t* base, int64_t rows, int64_t width
   return fn(map, swizzled ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<uint8_t*>(base), dims, strides, box, estr,
             CU_TENSOR_MAP_INTERLEAVE_NONE, swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool LONG>
+int launch(const Params& p, int64_t blocks, cudaStream_t s) {
+  static DeviceFlags smem_set;                      // per instantiation, per device
+  if (set_max_dynamic_smem(smem_set, gemm_fp8_few_kernel<LONG>, kSmemBytes) != cudaSuccess) return NVFP4_ERR_CUDA;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = p.split; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = kSmemBytes; cfg.stream = s;
+  cfg.attrs = attr; cfg.numAttrs = p.split > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, gemm_fp8_few_kernel<LONG>, p) == cudaSuccess ? NVFP4_OK : NVFP4_ERR_CUDA;
 }
 
 }  // namespace
@@ -479,17 +504,7 @@ int gemm_fp8_few(const Fp8Product& c, cudaStream_t s) {
     if ((p.k_stages - p.k_stages / p.split) * 14 <= 16 + p.M) p.split = 1;
     blocks = p.split > 1 ? (int64_t)p.tiles * p.split : std::min<int64_t>(p.tiles, sm_count());
   }
-  static DeviceFlags smem_set;
-  if (set_max_dynamic_smem(smem_set, gemm_fp8_few_kernel, kSmemBytes) != cudaSuccess) return NVFP4_ERR_CUDA;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = p.split; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)blocks); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = kSmemBytes; cfg.stream = s;
-  cfg.attrs = attr; cfg.numAttrs = p.split > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, gemm_fp8_few_kernel, p) == cudaSuccess ? NVFP4_OK : NVFP4_ERR_CUDA;
+  return ceil_div(p.k_stages, p.split) > kMostBlocks ? launch<true>(p, blocks, s) : launch<false>(p, blocks, s);
 }
 
 int fp8_few_error_word(unsigned int* out) {
