@@ -385,7 +385,8 @@ NVFP4_API int nvfp4_linear_fp8_bwd(const void* dY, const void* W, const void* X,
  * nvfp4_expert_sort: counts [experts] (slots of each expert, without padding), offsets [experts + 1], row_of [tokens * topk] (the
  *   slot's row, -1: dropped), slot_of [R] (the row's slot, -1: padding and unused rows); all int32.
  * nvfp4_expert_gather: rows[r] = w * x[token of r's slot], zero in padding; x [tokens, cols] with leading dimension ld, rows [R, cols].
- *   weights [tokens, topk] of weights_dtype, or NULL for 1.  Its gradient by x is nvfp4_expert_combine of the rows' gradient.
+ *   weights [tokens, topk] of weights_dtype, or NULL for 1.  Its gradient by x is nvfp4_expert_combine of the rows' gradient
+ *   with the same weights.
  * nvfp4_expert_combine: y[t] = sum over j of w[t,j] * rows[row of (t,j)], summed in fp32 in the order of j; dropped slots add nothing.
  * nvfp4_expert_combine_bwd: drows[r] = w * dy[token of r's slot] (zero in padding; NULL: not wanted), and
  *   dweights[t,j] = <dy[t], rows[row of (t,j)]> of weights_dtype, summed in fp32 (0 for a dropped slot).
@@ -418,7 +419,7 @@ NVFP4_API int nvfp4_expert_combine_bwd(const void* dy, int dtype, int64_t tokens
  *   rows' quantization, D [experts, N, K] dense.  An expert without rows gets zeros.
  * nvfp4_experts_fp8_fwd / _bwd: the layer: Y [R, N] from X; dX [R, K] and dW [experts, N, K] from dY, W and X.  x_by_token / dy_by_token and
  *   dy_weights as by_token and weights above (the weighted sum's output gradient goes in as it is).  Padding rows of Y and dX are
- *   zero.  N and K multiples of 8, everything dense and 16-byte aligned, workspace of nvfp4_experts_fp8_workspace_bytes(..., which) bytes as for nvfp4_linear_fp8_*.
+ *   zero (NaN where a block of the expert's weights holds a NaN or an infinity).  N and K multiples of 8, everything dense and 16-byte aligned, workspace of nvfp4_experts_fp8_workspace_bytes(..., which) bytes as for nvfp4_linear_fp8_*.
  */
 NVFP4_API int nvfp4_quantize_fp8_experts(const void* x, int dtype, int by_token, int64_t tokens, int64_t topk, int64_t experts, int64_t cols,
                                int64_t ld, const int32_t* offsets, const int32_t* slot_of, const void* weights, int weights_dtype,

@@ -1,15 +1,17 @@
 // Products of FP8 operands (fp8.cuh) with few rows of A: tokens on weights that are kept, and experts with few tokens each.
 //
-// Bound by the bytes of B, each read once.  gemm_fp8.cu's tiles would leave most multiprocessors idle (a CTA pair takes 256 columns of
+// Its floor is the bytes of B, each read once.  gemm_fp8.cu's tiles would leave most multiprocessors idle (a CTA pair takes 256 columns of
 // D) and fill half of their rings with rows that do not exist.  Here the operands change places: 128 rows of B (weights) are the
 // instruction's 128 rows, up to 128 rows of A (tokens), in steps of 16, its columns, so that nearly all of a k-stage of 128 values is
-// weights, and one block per multiprocessor keeps 160-190 KB of them in flight.  tcgen05.mma.cta_group::1.kind::mxf8f6f4, scales through
+// weights, of which a block keeps 160-190 KB in flight.  tcgen05.mma.cta_group::1.kind::mxf8f6f4, scales through
 // registers into tensor memory, a tile for four stages; a lane of the accumulator is a column of D, so that a warp stores 32 of a row at a
 // time.  us, weights that are in no cache (floor: their bytes at the rate of a copy): 11008 x 4096 (7.0) 1 row 12.0, 67 rows 13.0, 128 rows
 // 13.7; 4096 x 11008 (7.0) 11.6, 13.3, 14.9; 4096 x 4096 (2.6) 6.8, 8.9, 10.3.  With gemm_fp8.cu's kernel 15-16, 23, 11; with dot products by
-// mma.sync, 16 rows of B a block, 11.0, 15.2 and 7.3 for up to 8 rows, and twice that for 16.  About 3 us are a launch and the first and
-// last latencies; an instruction of 128 rows takes about 115 cycles however few its columns, but pairs of CTAs, whose instructions of
-// 256 rows take 40 to 64, gain nothing in all (11.8) and lose where clusters of eight blocks do not all find room (4096 x 11008 19.8).
+// mma.sync, 16 rows of B a block, 11.0, 15.2 and 7.3 for up to 8 rows, and twice that for 16.  3-4 us are a launch and the first and
+// last latencies.  The rest is the chain of a block's stages: an instruction of 128 rows takes about 115 cycles however few its columns, four of
+// them 0.25 us, and 11008 columns are 86 tiles, so that 86 of 148 multiprocessors go through 32 stages one after the other (8 us; two blocks
+// for a tile would be 172).  Pairs of CTAs, whose instructions of 256 rows take 40 to 64 cycles, gain nothing in all (11.8) and lose where
+// clusters of eight blocks do not all find room (4096 x 11008 19.8).
 //
 // One product: with few tiles of B a cluster of 2, 4 or 8 blocks shares one along the contraction axis; each then sums a share of
 // the tokens over all blocks' accumulators, which they write into one another's shared memory, in the order of the blocks.

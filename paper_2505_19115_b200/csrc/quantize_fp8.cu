@@ -9,12 +9,12 @@
 // half warp; transposed ones are packed along the thread's 8 rows and turned round in shared memory.  Nothing behind the last row or
 // column is written.
 // 8192 x 8192 bf16 (buffers in turn, nothing in the caches): row output 30 us = 6.7 TB/s, transposed 31 = 6.5, both 44 = 6.1; 16384 x
-// 11008 80 / 82 / 114 us = 6.7 / 6.6 / 6.3; fp32 8192 x 8192 50 / 54 / 65.  (A copy: 6.3-6.5 TB/s.)  Instructions come next: between
-// products that hold the clock down they decide (dY both ways, X^T and W^T of a 16384 x 11008 x 4096 layer 171 us alone, 206 there).  Hence
+// 11008 80 / 82 / 114 us = 6.7 / 6.6 / 6.3; fp32 8192 x 8192 50 / 54 / 65.  Blocks of 128 x 128 take no more: 8192 x 8192 30 (row) and
+// 43.5 (both), fp32 50 and 63, 11008 x 4096 20.6 and 30.0.  (A copy: 6.3-6.5 TB/s.)  Instructions come next: between products that hold the clock down they decide (dY both ways, X^T and W^T of a 16384 x 11008 x 4096 layer 171 us alone, 206 there).  Hence
 // the absence of branches around loads and, in tiles that are full, around stores, 32-bit tile indices without a division, and maxima that
 // stay packed until the last (12.3 a value for both outputs; 16.5 before the last three: 48, 182 and 242 us).  Transposed codes
 // moved 16 bytes at a time take fewer still, 11.4, and no less time.
-// 33000 rows of 2816 gathered from 16384, both outputs: 62 us, with weights 76.
+// 33000 rows of 2816 gathered from 16384, both outputs: 62 us, with weights 76 (with a fifth, or four fifths, of the tokens zero 75-76).
 #include <cuda_bf16.h>
 
 #include <type_traits>
@@ -269,7 +269,8 @@ __device__ __forceinline__ void finish_tile(const Fp8Op& op, int swizzled, const
     if (!(lane & 1)) store_scale(o.scales_r + b * op.sf_r, row + (l16 >> 1), op.rows, ct, op.col_tiles, swizzled, code);
     float own = fp8_scale_inverse(code);
     // A weight times a power of two is exact, so that one multiplication by both rounds as one by the weight; where it is not (numbers
-    // next to the smallest or the largest), the values are multiplied twice.
+    // next to the smallest or the largest; padding and other rows of zeros count as such), the warp multiplies its values twice, which
+    // takes at most 1 % more time.
     [[maybe_unused]] bool twice = false;
     if constexpr (WEIGHTED) {
       const float both = __fmul_rn(v.weight_mine, own);
