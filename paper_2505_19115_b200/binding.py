@@ -213,7 +213,7 @@ def _empty(size, dtype, like, stream):
     """An output of a call on `stream` (None: the current stream), on the device of the tensor `like`."""
     if stream is None:
         return torch.empty(size, dtype=dtype, device=like.device)
-    return _native().empty_on(stream, like, dtype, 1, *size)
+    return _native().empty_on(stream, like, dtype or torch.get_default_dtype(), 1, *size)
 
 
 def _scratch(nbytes, like, given, stream):
@@ -815,8 +815,9 @@ def nvfp4_microbench_mma_peak(stages: int, instr_n: int = 256, device=None, stre
     """Issue-rate measurement of the FP4 tensor-core instruction: returns an int64 tensor [pairs, 3] of
     (cycles, instructions, timed-out flag) per CTA pair."""
     dev = torch.device("cuda", torch.cuda.current_device()) if device is None else device
-    with torch.cuda.stream(stream):          # cleared there too
-        out = torch.zeros((torch.cuda.get_device_properties(dev).multi_processor_count // 2 + 1, 3), dtype=torch.int64, device=dev)
+    out = torch.zeros((torch.cuda.get_device_properties(dev).multi_processor_count // 2 + 1, 3), dtype=torch.int64, device=dev)
+    if stream is not None:
+        torch.cuda.current_stream(dev).synchronize()      # cleared before the kernel on that stream begins
     pairs = C.c_int(0)
     _check(lib().nvfp4_microbench_mma_peak(stages, instr_n, _ptr(out), out.numel() * 8, C.byref(pairs), _stream(stream)),
            "nvfp4_microbench_mma_peak")

@@ -19,6 +19,7 @@ def test_memory_on_a_given_stream_is_laid_out_as_asked():
         assert n.empty_fp8(like, 0, 130, 24, 1, 0, nb.SF_SWIZZLED, stream)[0].stride() == (32, 1)
         assert [t.shape for t in n.expert_buffers(like, 5, 2, 3, 256, stream)] == [(3,), (4,), (5, 2), (256,)]
     assert nb._empty((2, 3), torch.float32, like, Stream).shape == nb._empty((2, 3), torch.float32, like, None).shape == (2, 3)
+    assert nb._empty((2,), None, like, Stream).dtype == nb._empty((2,), None, like, None).dtype
     assert nb._scratch(1000, like, None, Stream).numel() == nb._scratch(1000, like, None, None).numel() == 1000
     assert nb._scratch(0, like, None, Stream).numel() == 256 and nb._scratch(1000, like, like, Stream) is like
 
