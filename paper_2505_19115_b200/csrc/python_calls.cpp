@@ -16,7 +16,9 @@
 //
 // Memory for a call that is given a stream is allocated on that stream (OnStream below): the allocator hands a block out again in the
 // order of the stream that it was allocated on, so that one of the current stream's could still be written by work queued there
-// earlier, or be given away while the call's kernels use it.
+// earlier, or be given away while the call's kernels use it.  Every output that is dropped then costs the host an event on the current
+// stream, about 2 us (one output 7.6 -> 9.2 us a call, four 7.1 -> 16.2); a caller who gives the outputs, or makes the stream the current
+// one, does not pay that.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -482,8 +484,8 @@ PyObject* py_bind(PyObject*, PyObject* args) {
 
 #define NVFP4_METHOD(name, ...) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr},
 #define NVFP4_HELPER(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {{"bind", py_bind, METH_VARARGS, nullptr}, NVFP4_HELPER(empty_fp8), NVFP4_HELPER(expert_buffers), NVFP4_HELPER(empty_rows), NVFP4_HELPER(empty_on), NVFP4_HELPER(fp8_operand),
-                         NVFP4_HELPER(quantize_fp8), NVFP4_HELPER(matrix), NVFP4_HELPER(dense),
+PyMethodDef methods[] = {{"bind", py_bind, METH_VARARGS, nullptr}, NVFP4_HELPER(empty_fp8), NVFP4_HELPER(expert_buffers), NVFP4_HELPER(empty_rows),
+                         NVFP4_HELPER(empty_on), NVFP4_HELPER(fp8_operand), NVFP4_HELPER(quantize_fp8), NVFP4_HELPER(matrix), NVFP4_HELPER(dense),
                          NVFP4_CALLS(NVFP4_METHOD) NVFP4_CALLS_HERE(NVFP4_METHOD){nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
