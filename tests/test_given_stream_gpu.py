@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 
 M, N, K = 256, 512, 768
 T, TOPK, E = 300, 2, 6
-PAUSE = 100_000_000                                  # cycles: about 50 ms, longer than everything that is queued behind it
+PAUSE = 300_000_000                                  # cycles: about 150 ms, longer than everything that is queued behind it
 
 
 def _x(shape, seed, std=1.0, dtype=torch.bfloat16):
@@ -147,7 +147,7 @@ def test_memory_of_a_call_is_not_written_by_work_queued_before_it(name, inputs):
     torch.cuda._sleep(PAUSE)
     for t in earlier:
         t.fill_(0x5A)
-    del earlier, t                                    # free on the current stream, written there in 50 ms
+    del earlier, t                                    # free on the current stream, written there in 150 ms
     got = _tensors(call(inputs, side))
     side.synchronize()
     assert not torch.cuda.current_stream().query()
@@ -166,7 +166,7 @@ def test_an_output_read_on_the_current_stream_and_dropped_is_not_written_by_the_
     places = [t.data_ptr() for t in got]
     torch.cuda.current_stream().wait_stream(side)
     torch.cuda._sleep(PAUSE)
-    read = [t.clone() for t in got]                   # in 50 ms
+    read = [t.clone() for t in got]                   # in 150 ms
     del got
     again = _tensors(call(inputs, side))              # the same bits, so that places are what tells
     assert not set(places) & {t.data_ptr() for t in again}
